@@ -8,15 +8,17 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
-SRC = os.path.join(PKG, "csrc", "runtime.hip")
+SRCS = [os.path.join(PKG, "csrc", f) for f in ("runtime.hip", "kv8.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libm2r2.so")
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-shared", "-fPIC",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # no packed fp32 instructions (v_pk_{add,mul,fma}_f32) anywhere
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-fvisibility=hidden",
@@ -30,9 +32,7 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found")
 
 
-def build(verbose: bool = False) -> str:
-    tmp = LIB + ".tmp"
-    cmd = [hipcc(), *HIPCC_FLAGS, "-I", INCLUDE, "-I", os.path.join(PKG, "csrc"), "-o", tmp, SRC]
+def _run(cmd, verbose: bool) -> None:
     if verbose:
         print(" ".join(cmd))
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -41,7 +41,19 @@ def build(verbose: bool = False) -> str:
         raise RuntimeError(f"hipcc failed ({r.returncode}):\n{msgs}")
     if verbose and msgs.strip():
         print(msgs)
-    os.replace(tmp, LIB)
+
+
+def build(verbose: bool = False) -> str:
+    """Compile every source side by side and link them."""
+    inc = ["-I", INCLUDE, "-I", os.path.join(PKG, "csrc")]
+    with tempfile.TemporaryDirectory(dir=PKG) as tmp:
+        objs = [os.path.join(tmp, os.path.basename(s) + ".o") for s in SRCS]
+        with ThreadPoolExecutor(len(SRCS)) as ex:
+            list(ex.map(lambda so: _run([hipcc(), *HIPCC_FLAGS, *inc, "-c", "-o", so[1], so[0]], verbose),
+                        zip(SRCS, objs)))
+        out = os.path.join(tmp, os.path.basename(LIB))
+        _run([hipcc(), *HIPCC_FLAGS, "-shared", "-o", out, *objs], verbose)
+        os.replace(out, LIB)
     return LIB
 
 

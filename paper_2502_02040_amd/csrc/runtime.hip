@@ -28,6 +28,7 @@
 #include "arla.h"
 #include "persist.h"
 #include "flops.h"
+#include "status.h"
 
 using namespace m2r2;
 
@@ -74,13 +75,18 @@ __global__ void k_fill_u32(uint32_t* p, int n, uint32_t v) {
 
 thread_local std::string g_err;
 
-m2r2_status fail(m2r2_status st, const char* fmt, ...) {
+m2r2_status vfail(m2r2_status st, const char* fmt, va_list ap) {
   char buf[512];
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  g_err = buf;
+  return st;
+}
+
+m2r2_status fail(m2r2_status st, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
-  vsnprintf(buf, sizeof buf, fmt, ap);
+  vfail(st, fmt, ap);
   va_end(ap);
-  g_err = buf;
   return st;
 }
 
@@ -356,6 +362,18 @@ m2r2_status check_config(const m2r2_config* c, int max_batch, int max_chunk, int
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 }  // namespace
+
+namespace m2r2 {
+
+m2r2_status set_error(m2r2_status st, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vfail(st, fmt, ap);
+  va_end(ap);
+  return st;
+}
+
+}  // namespace m2r2
 
 // Host side of the expert cache of a mixture-of-experts context.
 struct MoeState {

@@ -1,0 +1,193 @@
+"""ctypes binding of the 8-bit paged cache's operators (include/m2r2_kv8.h).
+
+Argument checks and marshalling only, as in ``binding``.  Tensors of one call
+are on one GPU; the call runs on that GPU's current stream unless one is
+given, whichever device is current.
+"""
+from __future__ import annotations
+
+import ctypes
+from ctypes import POINTER, c_float, c_int32, c_int64, c_size_t, c_void_p
+from typing import Optional
+
+from .binding import BF16, F32, _check, lib
+
+# include/m2r2_kv8.h
+KV8_EXPORTS = ("m2r2_kv8_append", "m2r2_kv8_workspace_size", "m2r2_kv8_attention")
+ERR_BLOCK, ERR_ROPE, ERR_ROWS = 2, 8, 32
+
+
+class _Pages(ctypes.Structure):
+    _fields_ = [("k_pages", c_void_p), ("v_pages", c_void_p), ("k_scales", c_void_p), ("v_scales", c_void_p),
+                ("block_table_d", c_void_p), ("num_blocks", c_int32), ("block_size", c_int32),
+                ("max_blocks_per_seq", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("n_seqs", c_int32), ("n_rows", c_int32), ("row_start_d", c_void_p), ("positions_d", c_void_p),
+                ("dtype", c_int32), ("k", c_void_p), ("v", c_void_p), ("k_row", c_int64), ("k_head", c_int64),
+                ("v_row", c_int64), ("v_head", c_int64), ("rope_d", c_void_p), ("rope_len", c_int32),
+                ("n_heads", c_int32), ("q", c_void_p), ("q_out", c_void_p), ("q_row", c_int64), ("q_head", c_int64),
+                ("qo_row", c_int64), ("qo_head", c_int64), ("err_d", c_void_p)]
+
+
+class _Query(ctypes.Structure):
+    _fields_ = [("n_seqs", c_int32), ("n_rows", c_int32), ("row_start_d", c_void_p), ("lens_d", c_void_p),
+                ("visible_d", c_void_p), ("dtype", c_int32), ("n_heads", c_int32), ("q", c_void_p),
+                ("q_row", c_int64), ("q_head", c_int64), ("own_d", c_void_p), ("own_k", c_void_p), ("own_v", c_void_p),
+                ("n_own", c_int32), ("ok_row", c_int64), ("ok_head", c_int64), ("ov_row", c_int64),
+                ("ov_head", c_int64), ("scale", c_float), ("out", c_void_p), ("out_row", c_int64),
+                ("out_head", c_int64), ("err_d", c_void_p)]
+
+
+_fns = None
+
+
+def _lib():
+    """(append, workspace size, attention) with their signatures set."""
+    global _fns
+    if _fns is None:
+        L = lib()
+        L.m2r2_kv8_append.argtypes = [POINTER(_Pages), POINTER(_Rows), c_void_p]
+        L.m2r2_kv8_workspace_size.argtypes = [POINTER(_Pages), c_int32, c_int32, c_int32, POINTER(c_size_t)]
+        L.m2r2_kv8_attention.argtypes = [POINTER(_Pages), POINTER(_Query), c_void_p, c_size_t, c_void_p]
+        for f in KV8_EXPORTS:
+            getattr(L, f).restype = c_int32
+        _fns = (L.m2r2_kv8_append, L.m2r2_kv8_workspace_size, L.m2r2_kv8_attention)
+    return _fns
+
+
+class KV8Pages:
+    """One layer of an 8-bit paged cache: ``k_pages``/``v_pages``
+    ``[num_blocks][n_kv_heads][block_size][head_dim]`` float8_e4m3fn codes,
+    ``k_scales``/``v_scales`` ``[num_blocks][n_kv_heads]`` float32 powers of two, and
+    the block table ``[n_seqs][max_blocks_per_seq]`` int32.  The tensors are the
+    caller's; a cached value is code * scale."""
+
+    def __init__(self, k_pages, v_pages, k_scales, v_scales, block_table):
+        import torch
+        if k_pages.dim() != 4 or k_pages.dtype != torch.float8_e4m3fn or not k_pages.is_contiguous():
+            raise ValueError("k_pages: a contiguous float8_e4m3fn tensor [blocks][heads][block size][head dim]")
+        for name, t, like in (("v_pages", v_pages, k_pages), ("v_scales", v_scales, k_scales)):
+            if t.shape != like.shape or t.dtype != like.dtype or not t.is_contiguous():
+                raise ValueError(f"{name}: contiguous, of the keys' shape and type")
+        if k_scales.shape != k_pages.shape[:2] or k_scales.dtype != torch.float32 or not k_scales.is_contiguous():
+            raise ValueError("k_scales: a contiguous float32 tensor [blocks][heads]")
+        if block_table.dim() != 2 or block_table.dtype != torch.int32 or not block_table.is_contiguous():
+            raise ValueError("block_table: a contiguous int32 tensor [sequences][blocks]")
+        self.device = k_pages.device
+        if any(t.device != self.device for t in (v_pages, k_scales, v_scales, block_table)):
+            raise ValueError("the cache's tensors are on different devices")
+        self.k_pages, self.v_pages, self.k_scales, self.v_scales = k_pages, v_pages, k_scales, v_scales
+        self.block_table = block_table
+        nb, H, bs, hd = k_pages.shape
+        self.n_seqs, self.n_kv_heads, self.head_dim = block_table.shape[0], H, hd
+        self._desc = _Pages(k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
+                            block_table.data_ptr(), nb, bs, block_table.shape[1], H, hd)
+
+
+def _int32s(t, n: Optional[int], name: str, device) -> Optional[int]:
+    import torch
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name}: a contiguous int32 vector on {device}")
+    if n is not None and t.shape[0] < n:
+        raise ValueError(f"{name}: {t.shape[0]} entries, {n} needed")
+    return t.data_ptr()
+
+
+def _rows(t, name: str, like, heads: int, kv: KV8Pages, n: Optional[int] = None):
+    """(pointer, row stride, head stride) of a [rows][heads][head_dim] tensor."""
+    sh, st = t.shape, t.stride()
+    if len(sh) != 3 or sh[1] != heads or sh[2] != kv.head_dim or st[2] != 1 or (n is not None and sh[0] != n):
+        raise ValueError(f"{name}: shape {tuple(sh)}, strides {tuple(st)}")
+    if t.dtype != like.dtype or t.device != kv.device:
+        raise ValueError(f"{name}: {t.dtype} on {t.device}")
+    return t.data_ptr(), st[0], st[1]
+
+
+def _dtype(t, name: str) -> int:
+    import torch
+    if t.dtype is torch.bfloat16:
+        return BF16
+    if t.dtype is torch.float32:
+        return F32
+    raise ValueError(f"{name}: {t.dtype} (bfloat16 or float32)")
+
+
+def _call(fn, where: str, device, stream, *args) -> None:
+    import torch
+    if device.type != "cuda":
+        raise ValueError(f"{where}: tensors on {device}")
+    s = (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+    if torch.cuda.current_device() == device.index:
+        _check(fn(*args, s), where)
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, s), where)
+
+
+def kv8_append(kv: KV8Pages, k, v, row_start, positions, *, rope=None, q=None, q_out=None, errors=None,
+               stream=None) -> None:
+    """Append rows ``k``/``v`` [rows][n_kv_heads][head_dim] to the cache: rows
+    row_start[s] .. row_start[s+1]-1 are sequence s's, from ``positions[s]`` on.
+    ``rope`` [length][head_dim/2][2] float32 (cos, sin) turns the keys (and the
+    queries ``q`` [rows][heads][head_dim] into ``q_out``, which may be ``q``).
+    ``errors``: an int32 tensor into which the kernels or error bits."""
+    import torch
+    n = k.shape[0]
+    pk = _rows(k, "k", k, kv.n_kv_heads, kv)
+    pv = _rows(v, "v", k, kv.n_kv_heads, kv, n)
+    heads, pq, po = 0, (None, 0, 0), (None, 0, 0)
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out come together")
+    if q is not None:
+        heads = q.shape[1]
+        pq, po = _rows(q, "q", k, heads, kv, n), _rows(q_out, "q_out", k, heads, kv, n)
+    rlen = 0
+    if rope is not None:
+        if (rope.dim() != 3 or rope.shape[1:] != (kv.head_dim // 2, 2) or rope.dtype is not torch.float32
+                or not rope.is_contiguous() or rope.device != kv.device):
+            raise ValueError("rope: a contiguous float32 tensor [length][head_dim/2][2]")
+        rlen = rope.shape[0]
+    ns = kv.n_seqs
+    r = _Rows(ns, n, _int32s(row_start, ns + 1, "row_start", kv.device), _int32s(positions, ns, "positions", kv.device),
+              _dtype(k, "k"), pk[0], pv[0], pk[1], pk[2], pv[1], pv[2], None if rope is None else rope.data_ptr(), rlen,
+              heads, pq[0], po[0], pq[1], pq[2], po[1], po[2], _int32s(errors, 1, "errors", kv.device))
+    _call(_lib()[0], "m2r2_kv8_append", kv.device, stream, kv._desc, r)
+
+
+def kv8_workspace(kv: KV8Pages, q):
+    """A zeroed workspace for ``kv8_attention`` calls of queries shaped like
+    ``q``, or smaller, over this cache.  Calls that may overlap need one each."""
+    import torch
+    n = c_size_t(0)
+    _check(_lib()[1](kv._desc, kv.n_seqs, q.shape[0], q.shape[1], n), "m2r2_kv8_workspace_size")
+    return torch.zeros(n.value, dtype=torch.uint8, device=kv.device)
+
+
+def kv8_attention(kv: KV8Pages, q, row_start, lens, out, workspace, *, visible=None, own=None, own_k=None, own_v=None,
+                  scale: Optional[float] = None, errors=None, stream=None) -> None:
+    """``out`` = softmax(scale * q K^T) V of rows ``q`` [rows][heads][head_dim]
+    over the first ``lens[s]`` positions of their sequences: row r sees
+    min(visible[r], lens[s]) of them (None: causal, the sequence's last row sees
+    all) and, where own[r] >= 0, the key and value own_k/own_v[own[r]] beside
+    them.  A row that sees nothing is zero."""
+    n, heads = q.shape[0], q.shape[1]
+    pq, po = _rows(q, "q", q, heads, kv), _rows(out, "out", q, heads, kv, n)
+    pk = pv = (None, 0, 0)
+    n_own = 0
+    if own is not None:
+        n_own = own_k.shape[0]
+        pk = _rows(own_k, "own_k", q, kv.n_kv_heads, kv)
+        pv = _rows(own_v, "own_v", q, kv.n_kv_heads, kv, n_own)
+    ns, dev = kv.n_seqs, kv.device
+    if workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace: a contiguous tensor on {dev}")
+    a = _Query(ns, n, _int32s(row_start, ns + 1, "row_start", dev), _int32s(lens, ns, "lens", dev),
+               _int32s(visible, n, "visible", dev), _dtype(q, "q"), heads, pq[0], pq[1], pq[2],
+               _int32s(own, n, "own", dev), pk[0], pv[0], n_own, pk[1], pk[2], pv[1], pv[2],
+               0.0 if scale is None else scale, po[0], po[1], po[2], _int32s(errors, 1, "errors", dev))
+    _call(_lib()[2], "m2r2_kv8_attention", dev, stream, kv._desc, a, workspace.data_ptr(),
+          workspace.numel() * workspace.element_size())
