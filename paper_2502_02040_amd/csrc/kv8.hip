@@ -2,9 +2,12 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
+#include <cmath>
 
 #include "kv8_append.h"
-#include "kv8_attn.h"
+#include "kv8_few.h"
+#include "kv8_many.h"
 #include "m2r2_kv8.h"
 #include "status.h"
 
@@ -78,10 +81,61 @@ void append_launch(const Kv8AppArgs& A, hipStream_t st) {
   else k8_append<BF, HD, 4, 4><<<(unsigned)units, kKv8AppThreads, 0, st>>>(A);
 }
 
+// How a call of attention is cut up.
+struct Cut {
+  bool many;       // k8_many
+  int cols;        // of a tile
+  int target;      // workgroups, about
+  int pcols;       // columns of a partial result
+  long long entries;
+  size_t bytes;    // of the workspace
+};
+
+// Sixteen columns a sequence on average and k8_few: more would read the cache
+// once for every sixteen.
+constexpr int kFewMost = 16;
+
+Cut cut(const m2r2_kv8* kv, int n_seqs, int n_rows, int n_heads) {
+  Cut c;
+  const int group = n_heads / kv->n_kv_heads, H = kv->n_kv_heads;
+  const long long cols = (long long)n_rows * group;
+  c.many = cols > (long long)kFewMost * std::max(1, n_seqs);
+  c.cols = c.many ? kManyCols : kFewCols;
+  c.target = c.many ? 512 : 1024;
+  c.pcols = (int)std::min<long long>(c.cols, std::max<long long>(1, cols));
+  const long long tiles = std::min<long long>(n_seqs, n_rows) + cols / c.cols;   // at most: ceil(a) <= a + 1 where a > 0
+  const long long cap = (long long)kv->max_blocks_per_seq * kv->block_size;
+  const long long most = tiles * std::min<long long>(kKv8MaxSplits, (cap + kKv8MinTokens - 1) / kKv8MinTokens);
+  c.entries = std::min(most, kv8_share(c.target, H) + tiles);
+  const long long slots = std::min(most, 2LL * kv8_share(c.target, H));
+  c.bytes = sizeof(uint32_t) * kKv8Counters + sizeof(float) * slots * H * kv8_part_floats(c.pcols, kv->head_dim);
+  return c;
+}
+
 template <int BF, int HD>
-void attn_launch(const Kv8AttnArgs& A, hipStream_t st) {
-  const long long waves = (long long)A.n_rows * A.n_heads;
-  k8_attn<BF, HD><<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(A);
+void few_launch(const Kv8AttnArgs& A, hipStream_t st) {
+  k8_few<BF, HD><<<(unsigned)(A.entries * A.kv.H), kFewThreads, 0, st>>>(A);
+}
+
+constexpr int kMaxDevices = 64;
+
+template <int BF, int HD>
+hipError_t many_setup() {   // LDS above 64 KB, once per device
+  static std::atomic<bool> done[kMaxDevices];
+  int dev = 0;
+  if (hipError_t e = hipGetDevice(&dev)) return e;
+  if (dev >= 0 && dev < kMaxDevices && done[dev].load(std::memory_order_acquire)) return hipSuccess;
+  const hipError_t e = hipFuncSetAttribute((const void*)&k8_many<BF, HD>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                           (int)sizeof(Kv8ManyLds<HD>));
+  if (e == hipSuccess && dev >= 0 && dev < kMaxDevices) done[dev].store(true, std::memory_order_release);
+  return e;
+}
+
+template <int BF, int HD>
+void many_launch(const Kv8AttnArgs& A, hipStream_t st, hipError_t* e) {
+  *e = many_setup<BF, HD>();
+  if (*e == hipSuccess)
+    k8_many<BF, HD><<<(unsigned)(A.entries * A.kv.H), kManyThreads, sizeof(Kv8ManyLds<HD>), st>>>(A);
 }
 
 #define M2R2_KV8_DISPATCH(FN, BFV, HDV, ...)                 \
@@ -142,7 +196,10 @@ M2R2_API m2r2_status m2r2_kv8_workspace_size(const m2r2_kv8* kv, int32_t n_seqs,
   if (n_seqs < 0 || n_rows < 0 || n_seqs > 1 << 20 || n_rows > 1 << 26)
     return set_error(M2R2_E_SHAPE, "n_seqs %d, n_rows %d", n_seqs, n_rows);
   if (!bytes_out) return set_error(M2R2_E_INVALID, "bytes_out is NULL");
-  *bytes_out = 256;
+  if ((long long)n_rows * n_heads >= 1LL << 31) return set_error(M2R2_E_SHAPE, "n_rows * n_heads reaches 2^31");
+  const Cut c = cut(kv, n_seqs, n_rows, n_heads);
+  if (c.entries * kv->n_kv_heads >= 1LL << 31) return set_error(M2R2_E_SHAPE, "too many rows and heads for one call");
+  *bytes_out = c.bytes;
   return M2R2_OK;
 }
 
@@ -178,7 +235,20 @@ M2R2_API m2r2_status m2r2_kv8_attention(const m2r2_kv8* kv, const m2r2_kv8_query
   A.n_own = a->own_d ? a->n_own : 0;
   A.scale = a->scale > 0.f ? a->scale : 1.f / sqrtf((float)kv->head_dim);
   A.err = a->err_d;
-  M2R2_KV8_DISPATCH(attn_launch, a->dtype == M2R2_BF16, kv->head_dim, A, stream);
+  A.group = a->n_heads / kv->n_kv_heads;
+  const Cut c = cut(kv, a->n_seqs, a->n_rows, a->n_heads);
+  A.cnt = (uint32_t*)workspace;
+  A.part = (float*)((char*)workspace + sizeof(uint32_t) * kKv8Counters);
+  A.pcols = c.pcols; A.target = c.target; A.entries = (int)c.entries;
+  const uint32_t d = kv->block_size / kKv8Slab;
+  A.bs_magic = ((1u << 31) + d - 1) / d;
+  if (c.many) {
+    hipError_t e = hipSuccess;
+    M2R2_KV8_DISPATCH(many_launch, a->dtype == M2R2_BF16, kv->head_dim, A, stream, &e);
+    if (e != hipSuccess) return set_error(M2R2_E_HIP, "m2r2_kv8_attention: %s", hipGetErrorString(e));
+  } else {
+    M2R2_KV8_DISPATCH(few_launch, a->dtype == M2R2_BF16, kv->head_dim, A, stream);
+  }
   return launched("m2r2_kv8_attention");
 }
 

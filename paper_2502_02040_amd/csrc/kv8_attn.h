@@ -1,4 +1,10 @@
-// Attention over the 8-bit paged cache: one wave per (row, query head).
+// Attention over the 8-bit paged cache: what its two kernels share.
+//
+// k8_few takes up to 16 columns (a row of a query head each) per workgroup
+// and is bound by the cache's bytes; k8_many takes 128 and is bound by the
+// matrix rate.  Both number their work alike: a sequence's columns of one
+// cache head are cut into tiles, its positions into splits, and the last split
+// of a tile to finish joins the partial results.
 #pragma once
 #include "kv8.h"
 
@@ -6,7 +12,7 @@ namespace m2r2 {
 
 struct Kv8AttnArgs {
   Kv8Pages kv;
-  int n_seqs, n_rows, n_heads;
+  int n_seqs, n_rows, n_heads, group;   // group: query heads of a cache head
   const int *row_start, *lens, *visible, *own;
   const void *q, *own_k, *own_v;
   void* out;
@@ -14,7 +20,195 @@ struct Kv8AttnArgs {
   int n_own;
   float scale;
   int* err;
+  uint32_t* cnt;     // arrivals of split tiles, zero between calls
+  float* part;       // partial results
+  int pcols;         // columns of a partial result
+  int target;        // workgroups that a launch is cut into, about
+  int entries;       // (tile, split) pairs that the grid covers
+  uint32_t bs_magic; // ceil(2^31 / (bs / 16))
 };
+
+constexpr int kKv8MaxSplits = 64;      // of a tile (the join's weights are in LDS)
+constexpr int kKv8MinTokens = 128;     // of a split, at least: a tile of 32 for each of four waves
+constexpr int kKv8Counters = 16384;    // split tiles of a call, at most
+
+// Splits and counters that a call can need.  A tile is split only if its
+// sequence is longer than W H / target positions, W the sum over tiles of
+// their sequences' lengths, so at most target / H tiles of a head are split,
+// into at most twice that many splits together.
+__host__ __device__ constexpr int kv8_share(int target, int heads) { return (target + heads - 1) / heads + 1; }
+
+typedef uint32_t u32x4_8_t __attribute__((ext_vector_type(4), aligned(8)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
+template <class T>
+__device__ __forceinline__ T kv8_ld(const void* p) {
+  return *(const __attribute__((address_space(1))) T*)p;
+}
+// A load at an address that is the same in all lanes, through the scalar cache
+// (nothing in the launch writes there).
+template <class T>
+__device__ __forceinline__ T kv8_lds(const T* p) {
+  return *(const __attribute__((address_space(4))) T*)p;
+}
+
+__device__ __forceinline__ uint32_t kv8_pk(float a, float b) {   // two bfloat16, nearest even
+  bf16x2_t r;
+  r[0] = (__bf16)a;
+  r[1] = (__bf16)b;
+  return __builtin_bit_cast(uint32_t, r);
+}
+
+// Codes 0, 1 (HI: 2, 3) of a word times a power of two, as two bfloat16 (exact).
+template <bool HI>
+__device__ __forceinline__ uint32_t kv8_up(uint32_t w, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HI));
+}
+
+// x as the sum of N bfloat16 parts (8, 16 or 24 significant bits).
+template <int N, bool FINITE = true>
+__device__ __forceinline__ void kv8_parts(const float (&x)[8], u32x4_t (&out)[N]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a = x[2 * i], b = x[2 * i + 1];
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+      const uint32_t w = kv8_pk(a, b);
+      out[p][i] = w;
+      a -= bf16lo(w);
+      b -= bf16hi(w);
+      if (!FINITE && p == 0) {   // an infinite value is its first part
+        if (!(fabsf(a) < INFINITY)) a = 0.f;
+        if (!(fabsf(b) < INFINITY)) b = 0.f;
+      }
+    }
+  }
+}
+
+// Bytes of a word that are NaN codes, as a mask of whole bytes.
+__device__ __forceinline__ uint32_t kv8_nan_bytes(uint32_t w) {
+  const uint32_t t = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+  return (t >> 7) * 0xffu;
+}
+
+__device__ __forceinline__ int kv8_wave_scan(int v) {   // inclusive sum
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(v, d);
+    v += lane >= d ? o : 0;
+  }
+  return v;
+}
+
+// One workgroup's piece of a call.
+struct Kv8Work {
+  int s, r0, cols, len;     // sequence, its first row, its columns (rows * group) and positions
+  int tile, split, splits;  // tile of columns; split of the positions
+  int t0, t1;               // the split's positions
+  int slot, unit;           // split tiles only: of its first partial result, of its counter
+};
+
+// Sequence s: columns and positions; no columns if row_start is not in order.
+template <int TC>
+__device__ __forceinline__ void kv8_seq(const Kv8AttnArgs& A, int s, bool report, int& r0, int& cols, int& len) {
+  r0 = A.row_start[s];
+  const int r1 = A.row_start[s + 1], l = A.lens[s];
+  const bool good = r0 >= 0 && r1 >= r0 && r1 <= A.n_rows;
+  const int64_t cap = (int64_t)A.kv.mbps * A.kv.bs;
+  if (report && !good) kv8_error(A.err, KV8_ERR_ROWS);
+  if (report && l > cap) kv8_error(A.err, KV8_ERR_BLOCK);
+  cols = good ? (r1 - r0) * A.group : 0;
+  len = (int)min((int64_t)max(l, 0), cap);
+}
+
+// Piece `entry` of the launch, the same in every wave.  Splits are as long as
+// an even share of all tiles' positions, so that sequences of very different
+// lengths keep every compute unit busy to the end.
+template <int TC>
+__device__ __forceinline__ bool kv8_pick(const Kv8AttnArgs& A, int entry, bool report, Kv8Work& w) {
+  const int lane = threadIdx.x & 63;
+  float sum = 0.f;
+  for (int c = 0; c < A.n_seqs; c += 64) {
+    int r0, cols, len;
+    kv8_seq<TC>(A, min(c + lane, A.n_seqs - 1), report && c + lane < A.n_seqs, r0, cols, len);
+    if (c + lane < A.n_seqs) sum += (float)((cols + TC - 1) / TC) * (float)len;
+  }
+  sum = wave_sum(sum);
+  // (a little more than the share: the float sum may be that much too small)
+  const float share = sum * (float)A.kv.H / (float)A.target * 1.002f;
+  const int per = max(kKv8MinTokens, ((int)min(share, 1e9f) / 64 + 1) * 64);
+  int before = 0, slots = 0, units = 0;
+  w.s = -1;
+  for (int c = 0; c < A.n_seqs; c += 64) {
+    const int s = min(c + lane, A.n_seqs - 1);
+    int r0, cols, len;
+    kv8_seq<TC>(A, s, false, r0, cols, len);
+    const int tiles = c + lane < A.n_seqs ? (cols + TC - 1) / TC : 0;
+    const int p = max(per, ((len + kKv8MaxSplits - 1) / kKv8MaxSplits + 63) / 64 * 64);
+    const int splits = max(1, (len + p - 1) / p);
+    const int mine = tiles * splits, ms = splits > 1 ? mine : 0, mu = splits > 1 ? tiles : 0;
+    const int upto = kv8_wave_scan(mine), us = kv8_wave_scan(ms), uu = kv8_wave_scan(mu);
+    const uint64_t hit = __ballot(entry >= before + upto - mine && entry < before + upto);
+    if (hit) {
+      const int l = __ffsll((unsigned long long)hit) - 1;
+      w.s = c + l;
+      w.r0 = __shfl(r0, l);
+      w.cols = __shfl(cols, l);
+      w.len = __shfl(len, l);
+      w.splits = __shfl(splits, l);
+      const int j = entry - before - __shfl(upto - mine, l), pl = __shfl(p, l);
+      w.tile = j / w.splits;
+      w.split = j % w.splits;
+      w.t0 = min(w.len, w.split * pl);
+      w.t1 = min(w.len, w.t0 + pl);
+      w.slot = slots + __shfl(us - ms, l) + w.tile * w.splits;
+      w.unit = units + __shfl(uu - mu, l) + w.tile;
+    }
+    before += __shfl(upto, 63);
+    slots += __shfl(us, 63);
+    units += __shfl(uu, 63);
+  }
+  // row starts that overlap can ask for more than the grid holds: nothing is done then
+  if (before > A.entries) {
+    if (report && lane == 0) kv8_error(A.err, KV8_ERR_ROWS);
+    return false;
+  }
+  return w.s >= 0;
+}
+
+// Positions that column c of the tile's sequence sees.
+__device__ __forceinline__ int kv8_sees(const Kv8AttnArgs& A, const Kv8Work& w, int c) {
+  if (c >= w.cols) return 0;
+  const int i = c / A.group;
+  const int v = A.visible ? A.visible[w.r0 + i] : w.len - (w.cols / A.group - 1 - i);
+  return min(max(v, 0), w.len);
+}
+
+// Where the 16 positions of group t / 16 of a sequence lie: their first cache
+// row (of all heads' rows of the pool) and scales.  Everything is the same in all
+// lanes, so the loads are scalar ones and wait on a counter of their own.
+struct Kv8Place {
+  int row;       // -1: not in the pool
+  float ks, vs;
+};
+__device__ __forceinline__ int kv8_block(const Kv8AttnArgs& A, int s, int t, int& in) {
+  const uint32_t G = (uint32_t)t >> 4;
+  const uint32_t lb = (uint32_t)(((uint64_t)G * A.bs_magic) >> 31);
+  in = (int)(t & ~15) - (int)lb * A.kv.bs;
+  return kv8_lds(A.kv.bt + (int64_t)s * A.kv.mbps + min((int)lb, A.kv.mbps - 1));
+}
+__device__ __forceinline__ Kv8Place kv8_place(const Kv8AttnArgs& A, int h, int blk, int in) {
+  const bool ok = blk >= 0 && blk < A.kv.nb;
+  const int page = (ok ? blk : 0) * A.kv.H + h;
+  Kv8Place p;
+  p.row = ok ? page * A.kv.bs + in : -1;
+  p.ks = kv8_lds(A.kv.ks + page);
+  p.vs = kv8_lds(A.kv.vs + page);
+  return p;
+}
 
 template <int BF>
 __device__ __forceinline__ float kv8_elem(const void* p, int64_t at) {
@@ -22,73 +216,38 @@ __device__ __forceinline__ float kv8_elem(const void* p, int64_t at) {
   else return ((const float*)p)[at];
 }
 
-template <int BF, int HD>
-__global__ __launch_bounds__(256) void k8_attn(Kv8AttnArgs A) {
-  const int lane = threadIdx.x & 63;
-  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int row = (int)(w / A.n_heads), h = (int)(w % A.n_heads);
-  if (row >= A.n_rows) return;
-  const int s = kv8_find(A.n_seqs, row, [&](int i) { return A.row_start[i]; });
-  const int r0 = A.row_start[s], r1 = A.row_start[s + 1];
-  if (r0 < 0 || r1 < r0 || r1 > A.n_rows) {
-    if (lane == 0) kv8_error(A.err, KV8_ERR_ROWS);
-    return;
-  }
-  if (row < r0 || row >= r1) return;
-  const int len = A.lens[s];
-  const int64_t cap = (int64_t)A.kv.mbps * A.kv.bs;
-  if (len > cap && lane == 0) kv8_error(A.err, KV8_ERR_BLOCK);
-  const int n = (int)min((int64_t)max(len, 0), cap);
-  const int see = min(n, A.visible ? A.visible[row] : len - (r1 - 1 - row));
-  const int hk = h / (A.n_heads / A.kv.H);
-  const bool on0 = lane < HD, on1 = lane + 64 < HD;
-  const int64_t at = (int64_t)row * A.q_row + (int64_t)h * A.q_head + lane;
-  const float q0 = on0 ? kv8_elem<BF>(A.q, at) * A.scale : 0.f, q1 = on1 ? kv8_elem<BF>(A.q, at + 64) * A.scale : 0.f;
-  float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f;
-  auto add = [&](float k0, float k1, float v0, float v1) {
-    const float z = wave_sum(q0 * k0 + q1 * k1);
-    const float mn = fmaxf(m, z);
-    const float al = m == -INFINITY ? 0.f : __expf(m - mn), p = z == -INFINITY ? 0.f : __expf(z - mn);
-    m = mn;
-    l = l * al + p;
-    o0 = o0 * al + p * v0;
-    o1 = o1 * al + p * v1;
-  };
-  for (int t = 0; t < see; ++t) {
-    const int lb = t / A.kv.bs, blk = A.kv.bt[(int64_t)s * A.kv.mbps + lb];
-    if (blk < 0 || blk >= A.kv.nb) {
-      if (lane == 0) kv8_error(A.err, KV8_ERR_BLOCK);
-      continue;
+// N consecutive elements (a multiple of 8, 16-byte aligned) as float.
+template <int BF, int N>
+__device__ __forceinline__ void kv8_row(const void* p, int64_t at, float (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 8) {
+    if constexpr (BF) {
+      const u32x4_t w = kv8_ld<u32x4_t>((const uint16_t*)p + at + i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[i + 2 * j] = bf16lo(w[j]);
+        x[i + 2 * j + 1] = bf16hi(w[j]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const f32x4_t w = kv8_ld<f32x4_t>((const float*)p + at + i + 4 * j);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[i + 4 * j + k] = w[k];
+      }
     }
-    const int64_t page = (int64_t)blk * A.kv.H + hk;
-    const int64_t p = (page * A.kv.bs + (t - lb * A.kv.bs)) * HD + lane;
-    const float ks = A.kv.ks[page], vs = A.kv.vs[page];
-    const float k0 = on0 ? __builtin_amdgcn_cvt_f32_fp8(A.kv.k[p], 0) * ks : 0.f;
-    const float k1 = on1 ? __builtin_amdgcn_cvt_f32_fp8(A.kv.k[p + 64], 0) * ks : 0.f;
-    const float v0 = on0 ? __builtin_amdgcn_cvt_f32_fp8(A.kv.v[p], 0) * vs : 0.f;
-    const float v1 = on1 ? __builtin_amdgcn_cvt_f32_fp8(A.kv.v[p + 64], 0) * vs : 0.f;
-    add(k0, k1, v0, v1);
-  }
-  const int ow = A.own ? A.own[row] : -1;
-  if (ow >= A.n_own && lane == 0) kv8_error(A.err, KV8_ERR_ROWS);
-  if (ow >= 0 && ow < A.n_own) {
-    const int64_t pk = (int64_t)ow * A.ok_row + (int64_t)hk * A.ok_head + lane;
-    const int64_t pv = (int64_t)ow * A.ov_row + (int64_t)hk * A.ov_head + lane;
-    add(on0 ? kv8_elem<BF>(A.own_k, pk) : 0.f, on1 ? kv8_elem<BF>(A.own_k, pk + 64) : 0.f,
-        on0 ? kv8_elem<BF>(A.own_v, pv) : 0.f, on1 ? kv8_elem<BF>(A.own_v, pv + 64) : 0.f);
-  }
-  const int64_t to = (int64_t)row * A.out_row + (int64_t)h * A.out_head + lane;
-  const float inv = l != 0.f ? 1.f / l : 0.f;
-  const float a = l != 0.f ? o0 * inv : 0.f, b = l != 0.f ? o1 * inv : 0.f;
-  if constexpr (BF) {
-    __bf16* out = (__bf16*)A.out;
-    if (on0) out[to] = (__bf16)a;
-    if (on1) out[to + 64] = (__bf16)b;
-  } else {
-    float* out = (float*)A.out;
-    if (on0) out[to] = a;
-    if (on1) out[to + 64] = b;
   }
 }
+
+// Sum of an unnormalised result over its weight; nothing seen: zero.
+__device__ __forceinline__ float kv8_over(float a, float l) { return l != 0.f ? a / l : 0.f; }
+
+// Weight of a partial result with maximum m in one with maximum M (base 2);
+// `l` zero: it has seen nothing (NaN weights are kept).
+__device__ __forceinline__ float kv8_weight(float m, float l, float M) {
+  return l != 0.f ? __builtin_amdgcn_exp2f(m - M) : 0.f;
+}
+
+constexpr float kLog2e = 1.4426950408889634f;
 
 }  // namespace m2r2

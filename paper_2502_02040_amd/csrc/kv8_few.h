@@ -1,0 +1,407 @@
+// Attention over the 8-bit cache for few columns: decoding, dual-stream rows,
+// short chunks.
+//
+// What bounds it: the cache's bytes, read once for the 16 columns of a tile.
+// A wave takes tiles of 32 positions and keeps everything between a load and
+// its use in registers, with the next tile in flight; the workgroup meets once,
+// at the end.
+//   * S^T = K Q^T: keys are the A operand.  Row r = 4 a + b of the first product
+//     is position 8 a + b, of the second 8 a + 4 + b, so that lane (q, g) gets
+//     the scores of positions 8 g .. 8 g + 7 of column q, which is the B operand
+//     of O^T = V^T P^T as it stands.  Lane (m, g) reads HD / 4 consecutive
+//     bytes of two positions: the dims of a step are numbered to suit.
+//   * A lane reads 8 bytes (dims 8 n ..) of the eight positions of its group;
+//     byte permutes pair two positions' codes of a dim, which the conversion to
+//     bfloat16 takes, with the block's scale, in one instruction: codes times a
+//     power of two are exact there.
+//   * Block ids and scales are the same for all lanes: scalar loads, one tile
+//     further ahead, so that they hold up no vector load.
+// Queries are bfloat16 as given, or float32 cut into three parts (24 bits).
+// Probabilities are rounded to 16 bits (two parts) for bfloat16 rows and kept to 24
+// for float32 rows: the matrix pipe is idle enough that both are free.
+#pragma once
+#include "kv8_attn.h"
+
+namespace m2r2 {
+
+constexpr int kFewCols = 16;
+constexpr int kFewWaves = 4;
+constexpr int kFewThreads = 64 * kFewWaves;
+constexpr int kFewTile = 32;
+
+__device__ __forceinline__ f32x4_t kv8_mma16(u32x4_t a, u32x4_t b, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c,
+                                                 0, 0, 0);
+}
+// Maximum and sum over the lanes l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ float kv8_col_max(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float kv8_col_sum(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+template <int BF, int HD>
+struct Kv8Few {
+  static constexpr int NS = HD / 32;        // matrix steps of a score
+  static constexpr int ND = HD / 8;         // lanes that hold dims of the output
+  static constexpr int QN = BF ? 1 : 3, PN = BF ? 2 : 3;
+  struct Tile {
+    uint32_t k[2][2 * NS];   // the lane's bytes of two positions
+    u32x2_t v[8];
+  };
+  struct Blocks {            // of a tile's two groups of 16 positions
+    int b[2], in[2];
+  };
+  struct Places {
+    Kv8Place p[2];
+  };
+  u32x4_t q[NS][QN];
+  float m_run, l_run;
+  f32x4_t acc[8];            // dim 8 (4 g + i) + j of column q: acc[j][i]
+
+  __device__ __forceinline__ void init(const Kv8AttnArgs& A, const Kv8Work& w, int h, int c) {
+    const int g = (threadIdx.x & 63) >> 4;
+    float x[8 * NS];
+    const int cc = min(c, w.cols - 1);
+    kv8_row<BF>(A.q, (int64_t)(w.r0 + cc / A.group) * A.q_row + (int64_t)(h * A.group + cc % A.group) * A.q_head + g * (HD / 4), x);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = c < w.cols ? x[8 * s + i] : 0.f;
+      kv8_parts<QN, false>(y, q[s]);
+    }
+    m_run = -INFINITY;
+    l_run = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  static __device__ __forceinline__ Blocks blocks(const Kv8AttnArgs& A, int s, int t) {
+    Blocks b;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) b.b[i] = kv8_block(A, s, t + 16 * i, b.in[i]);
+    return b;
+  }
+  static __device__ __forceinline__ Places places(const Kv8AttnArgs& A, int h, const Blocks& b) {
+    Places p;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) p.p[i] = kv8_place(A, h, b.b[i], b.in[i]);
+    return p;
+  }
+  static __device__ __forceinline__ void load(const Kv8AttnArgs& A, const Places& p, Tile& t) {
+    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+    const int rk = max((m >> 3) ? p.p[1].row : p.p[0].row, 0), rv = max((g >> 1) ? p.p[1].row : p.p[0].row, 0);
+    const uint8_t* kp = A.kv.k + (int64_t)(rk + 8 * ((m >> 2) & 1) + (m & 3)) * HD + g * (HD / 4);
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+#pragma unroll
+      for (int x = 0; x < 2 * NS; x += 4) {
+        if (2 * NS - x >= 4) {
+          const u32x4_8_t d = kv8_ld<u32x4_8_t>(kp + a * 4 * HD + 4 * x);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) t.k[a][x + i] = d[i];
+        } else {
+          const u32x2_t d = kv8_ld<u32x2_t>(kp + a * 4 * HD + 4 * x);
+          t.k[a][x] = d[0];
+          t.k[a][x + 1] = d[1];
+        }
+      }
+    }
+    const uint8_t* vp = A.kv.v + (int64_t)(rv + 8 * (g & 1)) * HD + 8 * min(m, ND - 1);
+#pragma unroll
+    for (int x = 0; x < 8; ++x) t.v[x] = kv8_ld<u32x2_t>(vp + x * HD);
+  }
+
+  // Positions t .. t+31.  FULL: every live column sees all of them; else
+  // column q sees those below `sees`, and none at or above `most` is seen by any.
+  template <bool FULL>
+  __device__ __forceinline__ void tile(Tile& t, const Places& pl, float c, int sees, int most) {
+    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+    const float ks = (m >> 3) ? pl.p[1].ks : pl.p[0].ks, vs = (g >> 1) ? pl.p[1].vs : pl.p[0].vs;
+    f32x4_t s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+    u32x4_t k0[NS], k1[NS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      k0[s] = u32x4_t{kv8_up<false>(t.k[0][2 * s], ks), kv8_up<true>(t.k[0][2 * s], ks),
+                      kv8_up<false>(t.k[0][2 * s + 1], ks), kv8_up<true>(t.k[0][2 * s + 1], ks)};
+      k1[s] = u32x4_t{kv8_up<false>(t.k[1][2 * s], ks), kv8_up<true>(t.k[1][2 * s], ks),
+                      kv8_up<false>(t.k[1][2 * s + 1], ks), kv8_up<true>(t.k[1][2 * s + 1], ks)};
+    }
+#pragma unroll
+    for (int p = QN - 1; p >= 0; --p)
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        s0 = kv8_mma16(k0[s], q[s][p], s0);
+        s1 = kv8_mma16(k1[s], q[s][p], s1);
+      }
+    float z[8], mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      z[i] = (i < 4 ? s0[i & 3] : s1[i & 3]) * c;
+      if (!FULL && 8 * g + i >= sees) z[i] = -INFINITY;
+      mx = fmaxf(mx, z[i]);
+    }
+    const float mn = fmaxf(m_run, kv8_col_max(mx));
+    const float mb = mn == -INFINITY ? 0.f : mn;   // (nothing seen yet)
+    const float al = __builtin_amdgcn_exp2f(m_run - mb);
+    m_run = mn;
+    float p[8], ls = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(z[i] - mb);
+      ls += p[i];
+    }
+    l_run = l_run * al + ls;
+    if (__any(al != 1.f)) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] *= al;
+    }
+    u32x4_t pp[PN];
+    kv8_parts<PN>(p, pp);
+    if constexpr (!FULL) {
+      // codes that some column does not see must not reach it: NaN becomes
+      // zero in the operand, and is added to the columns that see it
+      bool odd = false;
+      uint32_t ix[8], iy[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const bool live = 8 * g + x < most;
+        ix[x] = live ? kv8_nan_bytes(t.v[x][0]) : 0u;
+        iy[x] = live ? kv8_nan_bytes(t.v[x][1]) : 0u;
+        odd |= (ix[x] | iy[x]) != 0u;
+        t.v[x][0] = live ? t.v[x][0] & ~ix[x] : 0u;
+        t.v[x][1] = live ? t.v[x][1] & ~iy[x] : 0u;
+      }
+      if (__any(odd)) {
+        u32x4_t seen;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          seen[i] = (8 * g + 2 * i < sees ? 0x3f80u : 0u) | (8 * g + 2 * i + 1 < sees ? 0x3f800000u : 0u);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          u32x4_t one;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t a = (j < 4 ? ix[2 * i] : iy[2 * i]) >> (8 * (j & 3)), b = (j < 4 ? ix[2 * i + 1] : iy[2 * i + 1]) >> (8 * (j & 3));
+            one[i] = ((a & 0xffu) ? 0x3f80u : 0u) | ((b & 0xffu) ? 0x3f800000u : 0u);
+          }
+          const f32x4_t n = kv8_mma16(one, seen, f32x4_t{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (n[i] > 0.f) acc[j][i] = __uint_as_float(0x7fc00000u);
+        }
+      }
+    }
+    u32x4_t vt[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const uint32_t a = __builtin_amdgcn_perm(t.v[2 * i + 1][x], t.v[2 * i][x], 0x05010400u);
+        const uint32_t b = __builtin_amdgcn_perm(t.v[2 * i + 1][x], t.v[2 * i][x], 0x07030602u);
+        vt[4 * x][i] = kv8_up<false>(a, vs);
+        vt[4 * x + 1][i] = kv8_up<true>(a, vs);
+        vt[4 * x + 2][i] = kv8_up<false>(b, vs);
+        vt[4 * x + 3][i] = kv8_up<true>(b, vs);
+      }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int x = PN - 1; x >= 0; --x) acc[j] = kv8_mma16(vt[j], pp[x], acc[j]);
+  }
+
+  __device__ __forceinline__ void store(float* m, float* l, float* out) {
+    const int g = (threadIdx.x & 63) >> 4;
+    const float ls = kv8_col_sum(l_run);
+    if (g == 0) {
+      *m = m_run;
+      *l = ls;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int n = 4 * g + i;
+      if (n < ND) {
+        *(float4*)(out + 8 * n) = make_float4(acc[0][i], acc[1][i], acc[2][i], acc[3][i]);
+        *(float4*)(out + 8 * n + 4) = make_float4(acc[4][i], acc[5][i], acc[6][i], acc[7][i]);
+      }
+    }
+  }
+};
+
+// Floats of a partial result: the columns' accumulators, then their maxima and sums.
+__host__ __device__ constexpr int kv8_part_floats(int cols, int hd) { return cols * (hd + 2); }
+
+template <int BF>
+__device__ __forceinline__ void kv8_emit(const Kv8AttnArgs& A, int row, int head, int d, float v) {
+  const int64_t to = (int64_t)row * A.out_row + (int64_t)head * A.out_head + d;
+  if constexpr (BF) ((__bf16*)A.out)[to] = (__bf16)v;
+  else ((float*)A.out)[to] = v;
+}
+
+template <int BF, int HD>
+__global__ __launch_bounds__(kFewThreads, 2) void k8_few(Kv8AttnArgs A) {
+  using F = Kv8Few<BF, HD>;
+  constexpr int OD = HD / 16;   // dims of a thread of the own keys
+  __shared__ __attribute__((aligned(16))) float acc_s[kFewWaves][kFewCols][HD];
+  __shared__ float m_s[kFewWaves][kFewCols], l_s[kFewWaves][kFewCols];
+  __shared__ float ov_s[kFewCols][HD], oz_s[kFewCols];   // own values and scores (first split)
+  __shared__ float mw[kFewCols][kKv8MaxSplits], lw[kFewCols][kKv8MaxSplits], li_s[kFewCols];
+  __shared__ int last_s;
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int h = blockIdx.x % A.kv.H, entry = blockIdx.x / A.kv.H;
+  Kv8Work w;
+  if (!kv8_pick<kFewCols>(A, entry, blockIdx.x == 0 && wv == 0, w)) return;
+  // (uniform: the loads that depend on them are scalar)
+  w.s = __builtin_amdgcn_readfirstlane(w.s);
+  w.t0 = __builtin_amdgcn_readfirstlane(w.t0);
+  w.t1 = __builtin_amdgcn_readfirstlane(w.t1);
+  const int c0 = w.tile * kFewCols, live = min(kFewCols, w.cols - c0);
+  const int q = lane & 15, c = c0 + q;
+  const int sees = kv8_sees(A, w, c);
+  // positions that any, and that every live column sees
+  int most = sees, least = q < live ? sees : 1 << 30;
+#pragma unroll
+  for (int d = 1; d < 16; d <<= 1) {
+    most = max(most, __shfl_xor(most, d));
+    least = min(least, __shfl_xor(least, d));
+  }
+  most = __builtin_amdgcn_readfirstlane(most);
+  least = __builtin_amdgcn_readfirstlane(least);
+  const int t1 = min(w.t1, most);
+  const int ntile = t1 > w.t0 ? (t1 - w.t0 + kFewTile - 1) / kFewTile : 0;
+  const float sc = A.scale * kLog2e;
+  F f;
+  typename F::Tile ta, tb;
+  typename F::Places pa, pb;
+  typename F::Blocks bn;
+  auto at = [&](int tt) { return w.t0 + min(tt, max(ntile - 1, 0)) * kFewTile; };
+  int tt = wv;
+  if (tt < ntile) {
+    pa = F::places(A, h, F::blocks(A, w.s, at(tt)));
+    F::load(A, pa, ta);
+    bn = F::blocks(A, w.s, at(tt + kFewWaves));
+  }
+  // own keys and values: 16 threads per column
+  const bool own = A.own && w.split == 0;
+  if (own) {
+    const int oc = tid >> 4, part = tid & 15, cc = min(c0 + oc, w.cols - 1);
+    const int row = w.r0 + cc / A.group;
+    const int o = oc < live ? A.own[row] : -1;
+    if (o >= A.n_own && part == 0) kv8_error(A.err, KV8_ERR_ROWS);
+    const bool has = o >= 0 && o < A.n_own;
+    float z = 0.f;
+    if (has) {
+      const int64_t qa = (int64_t)row * A.q_row + (int64_t)(h * A.group + cc % A.group) * A.q_head + part * OD;
+      const int64_t ka = (int64_t)o * A.ok_row + (int64_t)h * A.ok_head + part * OD;
+      const int64_t va = (int64_t)o * A.ov_row + (int64_t)h * A.ov_head + part * OD;
+#pragma unroll
+      for (int d = 0; d < OD; ++d) {
+        z += kv8_elem<BF>(A.q, qa + d) * kv8_elem<BF>(A.own_k, ka + d);
+        ov_s[oc][part * OD + d] = kv8_elem<BF>(A.own_v, va + d);
+      }
+    }
+    z = row_sum16(z) * sc;
+    if (part == 0) oz_s[oc] = has ? z : -INFINITY;
+  }
+  f.init(A, w, h, c);
+  auto step = [&](typename F::Tile& t, const typename F::Places& p) {
+    const int t0 = w.t0 + tt * kFewTile;
+    const bool ok = p.p[0].row >= 0 && p.p[1].row >= 0;
+    if (t0 + kFewTile <= least && ok) {
+      f.template tile<true>(t, p, sc, 0, 0);
+    } else {
+      // (a group outside the pool is not seen)
+      const int g = lane >> 4;
+      const bool gone = p.p[g >> 1].row < 0;
+      const bool gap = t0 + 16 * (g >> 1) < most && gone;
+      if (gap && (lane & 15) == 0) kv8_error(A.err, KV8_ERR_BLOCK);
+      f.template tile<false>(t, p, sc, gone ? 0 : min(sees, t1) - t0, gone ? 0 : t1 - t0);
+    }
+  };
+  while (tt < ntile) {
+    pb = F::places(A, h, bn);
+    if (tt + kFewWaves < ntile) F::load(A, pb, tb);
+    bn = F::blocks(A, w.s, at(tt + 2 * kFewWaves));
+    step(ta, pa);
+    tt += kFewWaves;
+    if (tt >= ntile) break;
+    pa = F::places(A, h, bn);
+    if (tt + kFewWaves < ntile) F::load(A, pa, ta);
+    bn = F::blocks(A, w.s, at(tt + 2 * kFewWaves));
+    step(tb, pb);
+    tt += kFewWaves;
+  }
+  f.store(&m_s[wv][q], &l_s[wv][q], acc_s[wv][q]);
+  __syncthreads();
+  // ---- the waves' results, and the own key's, combined -------------------------
+  float* part = A.part + ((int64_t)w.slot * A.kv.H + h) * kv8_part_floats(A.pcols, HD);
+  const int64_t pstep = (int64_t)A.kv.H * kv8_part_floats(A.pcols, HD);
+  for (int e = tid; e < live * HD; e += kFewThreads) {
+    const int i = e / HD, d = e % HD;
+    const float oz = own ? oz_s[i] : -INFINITY;
+    float M = oz;
+#pragma unroll
+    for (int x = 0; x < kFewWaves; ++x) M = fmaxf(M, m_s[x][i]);
+    float l = oz != -INFINITY ? __builtin_amdgcn_exp2f(oz - M) : 0.f;
+    float a = l != 0.f ? l * ov_s[i][d] : 0.f;
+#pragma unroll
+    for (int x = 0; x < kFewWaves; ++x) {
+      const float y = kv8_weight(m_s[x][i], l_s[x][i], M);
+      if (l_s[x][i] != 0.f) {
+        a += y * acc_s[x][i][d];
+        l += y * l_s[x][i];
+      }
+    }
+    if (w.splits == 1) {
+      kv8_emit<BF>(A, w.r0 + (c0 + i) / A.group, h * A.group + (c0 + i) % A.group, d, kv8_over(a, l));
+    } else {
+      float* p = part + (int64_t)w.split * pstep;
+      st_agent(p + e, a);
+      if (d == 0) {
+        st_agent(p + A.pcols * HD + 2 * i, M);
+        st_agent(p + A.pcols * HD + 2 * i + 1, l);
+      }
+    }
+  }
+  if (w.splits == 1) return;
+  // ---- the last split to arrive joins them ---------------------------------------
+  if (!arrive_last(A.cnt + w.unit * A.kv.H + h, w.splits, &last_s)) return;
+  for (int e = tid; e < live * w.splits; e += kFewThreads) {
+    const int i = e / w.splits, x = e % w.splits;
+    const float* p = part + (int64_t)x * pstep + A.pcols * HD + 2 * i;
+    mw[i][x] = ld_agent(p);
+    lw[i][x] = ld_agent(p + 1);
+  }
+  __syncthreads();
+  if (tid < live) {
+    float M = -INFINITY, l = 0.f;
+    for (int x = 0; x < w.splits; ++x) M = fmaxf(M, mw[tid][x]);
+    for (int x = 0; x < w.splits; ++x) {
+      const float y = kv8_weight(mw[tid][x], lw[tid][x], M);
+      mw[tid][x] = y;
+      if (lw[tid][x] != 0.f) l += y * lw[tid][x];
+    }
+    li_s[tid] = l;
+  }
+  __syncthreads();
+  for (int e = tid; e < live * HD; e += kFewThreads) {
+    const int i = e / HD, d = e % HD;
+    float a = 0.f;
+#pragma unroll 16
+    for (int x = 0; x < w.splits; ++x) {
+      const float v = ld_agent(part + (int64_t)x * pstep + e);
+      if (lw[i][x] != 0.f) a += mw[i][x] * v;
+    }
+    kv8_emit<BF>(A, w.r0 + (c0 + i) / A.group, h * A.group + (c0 + i) % A.group, d, kv8_over(a, li_s[i]));
+  }
+}
+
+}  // namespace m2r2

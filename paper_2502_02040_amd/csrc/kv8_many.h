@@ -1,0 +1,401 @@
+// Attention over the 8-bit cache for many columns: prompts and pieces of them.
+//
+// What bounds it: the matrix rate, and beside it the exponentials and the LDS.
+// A workgroup holds 128 columns (32 a wave) and stages tiles of 64 positions:
+// codes are converted to bfloat16 (exactly: code times a power of two) and
+// values transposed once for all four waves.  The codes of the next tile are in
+// registers, those of the one after in flight; two buffers in LDS, one barrier
+// per tile.
+//   * S^T = K Q^T in 32 x 32 products.  Row m of a product is position
+//     16 (m / 16) + 8 (m / 4 % 2) + 4 (m / 8 % 2) + m % 4 of its half, so that lane
+//     (column, hi) gets the scores of positions 16 u + 8 hi .. + 7, which is the B
+//     operand of O^T = V^T P^T as it stands.
+//   * Two workgroups per compute unit, so that one's softmax runs beside the
+//     other's products.
+// Probabilities of bfloat16 rows are rounded to bfloat16 (half a step of 2^-8, of
+// the same size as the result's own rounding, and averaged over the positions):
+// a second part would cost half of all products again.  Those of float32 rows
+// are kept to 24 bits.
+#pragma once
+#include "kv8_few.h"
+
+namespace m2r2 {
+
+constexpr int kManyCols = 128;
+constexpr int kManyTile = 64;
+constexpr int kManyThreads = 256;
+
+template <int HD>
+struct Kv8ManyLds {
+  static constexpr int KP = HD + 8;           // padded rows (elements): 16 lanes' 16 bytes hit all banks
+  static constexpr int VP = kManyTile + 8;
+  uint16_t k[2][kManyTile * KP];              // [position][dim]
+  uint16_t v[2][HD * VP];                     // [dim][position]
+  // of a tile (four in turn): positions outside the pool; whether a value is NaN that not all columns see
+  unsigned long long gap[4];
+  int odd[4];
+  int last;
+};
+
+__device__ __forceinline__ f32x16_t kv8_mma32(u32x4_t a, u32x4_t b, f32x16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c,
+                                                 0, 0, 0);
+}
+__device__ __forceinline__ float kv8_swap32(float v) {   // the other half's value
+  return __shfl_xor(v, 32);
+}
+
+template <int BF, int HD>
+__global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs A) {
+  constexpr int NQ = HD / 16;                // matrix steps of a score
+  constexpr int NO = HD / 32;                // tiles of 32 output dims
+  constexpr int QN = BF ? 1 : 3, PN = BF ? 1 : 3;
+  using L = Kv8ManyLds<HD>;
+  constexpr int KP = L::KP, VP = L::VP;
+  constexpr int NK = HD / 32;                // 8-byte pieces of keys per thread: positions 4 threads each
+  constexpr int ND = HD / 8;                 // groups of 8 dims: values are staged by 16 ND threads
+  extern __shared__ __attribute__((aligned(16))) char lds_raw[];
+  L& S = *(L*)lds_raw;
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, hi = lane >> 5;
+  const int h = blockIdx.x % A.kv.H, entry = blockIdx.x / A.kv.H;
+  Kv8Work w;
+  if (!kv8_pick<kManyCols>(A, entry, blockIdx.x == 0 && wv == 0, w)) return;
+  w.s = __builtin_amdgcn_readfirstlane(w.s);
+  w.t0 = __builtin_amdgcn_readfirstlane(w.t0);
+  w.t1 = __builtin_amdgcn_readfirstlane(w.t1);
+  const int c0 = w.tile * kManyCols, c = c0 + 32 * wv + n;
+  const bool live = c < w.cols;
+  const int cc = min(c, w.cols - 1);
+  const int row = w.r0 + cc / A.group, head = h * A.group + cc % A.group;
+  const int sees = kv8_sees(A, w, c);
+  // of the wave's columns, and of the workgroup's (a tile's 128 columns: every thread looks at all)
+  int most = sees, least = live ? sees : 1 << 30;
+  int most_all = 0, least_all = 1 << 30;
+#pragma unroll
+  for (int x = 0; x < kManyCols / 64; ++x) {
+    const int o = c0 + 64 * x + lane, v = kv8_sees(A, w, o);
+    most_all = max(most_all, v);
+    least_all = min(least_all, o < w.cols ? v : 1 << 30);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    most = max(most, __shfl_xor(most, d));
+    least = min(least, __shfl_xor(least, d));
+    most_all = max(most_all, __shfl_xor(most_all, d));
+    least_all = min(least_all, __shfl_xor(least_all, d));
+  }
+  most = __builtin_amdgcn_readfirstlane(most);
+  least = __builtin_amdgcn_readfirstlane(least);
+  most_all = __builtin_amdgcn_readfirstlane(most_all);
+  least_all = __builtin_amdgcn_readfirstlane(least_all);
+  const int t1 = min(w.t1, most_all);
+  const int ntile = t1 > w.t0 ? (t1 - w.t0 + kManyTile - 1) / kManyTile : 0;
+  const float sc = A.scale * kLog2e;
+
+  // ---- staging ------------------------------------------------------------------
+  // keys: thread (position tid / 4, part tid % 4) takes HD / 4 bytes; values:
+  // thread (positions 4 (tid % 16) .., dims 8 (tid / 16) ..) takes 4 x 8 bytes
+  const int kt = tid >> 2, kd = (tid & 3) * (HD / 4), vt = (tid & 15) * 4, vd = (tid >> 4) * 8;
+  struct Raw {
+    u32x2_t k[NK], v[4];
+    float ks, vs;
+    bool kok, vok;   // the place exists
+  };
+  auto fetch = [&](int tt, Raw& r) {
+    const int t = w.t0 + tt * kManyTile;
+    auto place = [&](int tp, int& rw, bool& ok) {   // per lane
+      int in;
+      const uint32_t G = (uint32_t)tp >> 4;
+      const uint32_t lb = (uint32_t)(((uint64_t)G * A.bs_magic) >> 31);
+      in = tp - (int)lb * A.kv.bs;
+      const int blk = A.kv.bt[(int64_t)w.s * A.kv.mbps + min((int)lb, A.kv.mbps - 1)];
+      ok = blk >= 0 && blk < A.kv.nb;
+      if (!ok && tp < t1) kv8_error(A.err, KV8_ERR_BLOCK);
+      const int page = (ok ? blk : 0) * A.kv.H + h;
+      rw = page * A.kv.bs + in;
+      return page;
+    };
+    int rk, rv;
+    const int pk = place(t + kt, rk, r.kok), pv = place(t + vt, rv, r.vok);
+    r.ks = A.kv.ks[pk];
+    r.vs = A.kv.vs[pv];
+    const uint8_t* kp = A.kv.k + (int64_t)rk * HD + kd;
+#pragma unroll
+    for (int x = 0; x < NK; ++x) r.k[x] = kv8_ld<u32x2_t>(kp + 8 * x);
+    const uint8_t* vp = A.kv.v + (int64_t)rv * HD + min(vd, HD - 8);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) r.v[x] = kv8_ld<u32x2_t>(vp + x * HD);
+  };
+  auto stage = [&](int tt, Raw& r, int buf) {
+    const int t = w.t0 + tt * kManyTile;
+    if (tid == 0) {   // marks that were last read two tiles ago
+      S.gap[(tt + 2) & 3] = 0;
+      S.odd[(tt + 2) & 3] = 0;
+    }
+    if (!r.kok) atomicOr(&S.gap[tt & 3], 1ull << kt);
+#pragma unroll
+    for (int x = 0; x < NK; ++x) {
+      const u32x4_t o = {kv8_up<false>(r.k[x][0], r.ks), kv8_up<true>(r.k[x][0], r.ks), kv8_up<false>(r.k[x][1], r.ks),
+                         kv8_up<true>(r.k[x][1], r.ks)};
+      *(u32x4_t*)&S.k[buf][kt * KP + kd + 8 * x] = o;
+    }
+    if (vd < HD) {
+      if (t + kManyTile > least_all || !r.vok) {
+        // what no column sees is zero; NaN that some see and some do not is looked for by the waves
+        bool odd = false;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const bool there = t + vt + x < t1 && r.vok;
+          r.v[x][0] = there ? r.v[x][0] : 0u;
+          r.v[x][1] = there ? r.v[x][1] : 0u;
+          odd |= (kv8_nan_bytes(r.v[x][0]) | kv8_nan_bytes(r.v[x][1])) != 0u;
+        }
+        if (odd) S.odd[tt & 3] = 1;
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        uint32_t o[4][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t a = __builtin_amdgcn_perm(r.v[2 * i + 1][x], r.v[2 * i][x], 0x05010400u);
+          const uint32_t b = __builtin_amdgcn_perm(r.v[2 * i + 1][x], r.v[2 * i][x], 0x07030602u);
+          o[0][i] = kv8_up<false>(a, r.vs);
+          o[1][i] = kv8_up<true>(a, r.vs);
+          o[2][i] = kv8_up<false>(b, r.vs);
+          o[3][i] = kv8_up<true>(b, r.vs);
+        }
+#pragma unroll
+        for (int d = 0; d < 4; ++d) *(u32x2_t*)&S.v[buf][(vd + 4 * x + d) * VP + vt] = u32x2_t{o[d][0], o[d][1]};
+      }
+    }
+  };
+
+  // ---- queries ----------------------------------------------------------------------
+  u32x4_t q[NQ][QN];
+#pragma unroll
+  for (int s = 0; s < NQ; ++s) {
+    float x[8];
+    kv8_row<BF>(A.q, (int64_t)row * A.q_row + (int64_t)head * A.q_head + 16 * s + 8 * hi, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = live ? x[i] : 0.f;
+    kv8_parts<QN, false>(x, q[s]);
+  }
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x16_t acc[NO];
+#pragma unroll
+  for (int d = 0; d < NO; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
+  if (tid < 4) {
+    S.gap[tid] = 0;
+    S.odd[tid] = 0;
+  }
+  __syncthreads();
+  Raw ra;
+  if (ntile > 0) {
+    fetch(0, ra);
+    stage(0, ra, 0);
+    if (ntile > 1) fetch(1, ra);
+  }
+  __syncthreads();
+  // row m of a product is this position of its 32
+  const int krow = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
+  for (int tt = 0; tt < ntile; ++tt) {
+    const int buf = tt & 1, t0 = w.t0 + tt * kManyTile;
+    if (t0 < most) {
+      const unsigned long long gap = S.gap[tt & 3] >> (8 * hi);
+      const bool full = t0 + kManyTile <= least && !__any(gap != 0);
+      f32x16_t sa[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sa[x][r] = 0.f;
+      }
+#pragma unroll
+      for (int s = 0; s < NQ; ++s) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const u32x4_t k = *(const u32x4_t*)&S.k[buf][(32 * x + krow) * KP + 16 * s + 8 * hi];
+#pragma unroll
+          for (int p = QN - 1; p >= 0; --p) sa[x] = kv8_mma32(k, q[s][p], sa[x]);
+        }
+      }
+      // lane (column n, hi): scores of positions 32 x + 16 (r / 8) + 8 hi + r % 8
+      float mx = -INFINITY;
+      if (full) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sa[x][r]);
+      } else {
+        const int lim = min(sees, t1) - t0 - 8 * hi;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int at = 32 * x + 16 * (r >> 3) + (r & 7);
+            if (at >= lim || ((gap >> at) & 1)) sa[x][r] = -INFINITY;
+            mx = fmaxf(mx, sa[x][r]);
+          }
+      }
+      mx = fmaxf(mx, kv8_swap32(mx)) * sc;
+      const float mn = fmaxf(m_run, mx);
+      const float mb = mn == -INFINITY ? 0.f : mn;
+      const float al = __builtin_amdgcn_exp2f(m_run - mb);
+      m_run = mn;
+      float ls = 0.f;
+      u32x4_t pb[4][PN];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        float p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sa[u >> 1][8 * (u & 1) + i], sc, -mb));
+          ls += p[i];
+        }
+        kv8_parts<PN>(p, pb[u]);
+      }
+      l_run = l_run * al + ls;
+      if (__any(al != 1.f)) {
+#pragma unroll
+        for (int d = 0; d < NO; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[d][r] *= al;
+      }
+      if (!full && S.odd[tt & 3]) {
+        // NaN values reach only the columns that see them
+        const int lim = min(sees, t1) - t0 - 8 * hi;
+#pragma unroll 1
+        for (int d = 0; d < NO; ++d) {
+          f32x16_t o = acc[d], bad;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) bad[r] = 0.f;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            u32x4_t v = *(const u32x4_t*)&S.v[buf][(32 * d + n) * VP + 16 * u + 8 * hi], one, seen;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const bool n0 = (v[i] & 0x7fffu) > 0x7f80u, n1 = ((v[i] >> 16) & 0x7fffu) > 0x7f80u;
+              one[i] = (n0 ? 0x3f80u : 0u) | (n1 ? 0x3f800000u : 0u);
+              v[i] &= (n0 ? 0u : 0xffffu) | (n1 ? 0u : 0xffff0000u);
+              seen[i] = (16 * u + 2 * i < lim ? 0x3f80u : 0u) | (16 * u + 2 * i + 1 < lim ? 0x3f800000u : 0u);
+            }
+            bad = kv8_mma32(one, seen, bad);
+#pragma unroll
+            for (int p = PN - 1; p >= 0; --p) o = kv8_mma32(v, pb[u][p], o);
+          }
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[r] = bad[r] > 0.f ? __uint_as_float(0x7fc00000u) : o[r];
+#pragma unroll
+          for (int e = 0; e < NO; ++e)
+            if (e == d) acc[e] = o;
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int d = 0; d < NO; ++d) {
+            const u32x4_t v = *(const u32x4_t*)&S.v[buf][(32 * d + n) * VP + 16 * u + 8 * hi];
+#pragma unroll
+            for (int p = PN - 1; p >= 0; --p) acc[d] = kv8_mma32(v, pb[u][p], acc[d]);
+          }
+      }
+    }
+    if (tt + 1 < ntile) {
+      // (the other buffer's readers passed the last barrier)
+      stage(tt + 1, ra, buf ^ 1);
+      if (tt + 2 < ntile) fetch(tt + 2, ra);
+      __syncthreads();
+    }
+  }
+  // ---- results -----------------------------------------------------------------------
+  // the own key, once
+  if (A.own && w.split == 0) {
+    const int o = live ? A.own[row] : -1;
+    if (o >= A.n_own && hi == 0) kv8_error(A.err, KV8_ERR_ROWS);
+    const bool has = o >= 0 && o < A.n_own;
+    float z = 0.f;
+    const int oo = has ? o : 0;
+#pragma unroll 4
+    for (int d = 0; d < HD / 2; ++d) {
+      const int dd = hi * (HD / 2) + d;
+      z += kv8_elem<BF>(A.q, (int64_t)row * A.q_row + (int64_t)head * A.q_head + dd) *
+           kv8_elem<BF>(A.own_k, (int64_t)oo * A.ok_row + (int64_t)h * A.ok_head + dd);
+    }
+    z = (z + kv8_swap32(z)) * sc;
+    if (!has) z = -INFINITY;
+    const float mn = fmaxf(m_run, z), mb = mn == -INFINITY ? 0.f : mn;
+    const float al = __builtin_amdgcn_exp2f(m_run - mb), p = has ? __builtin_amdgcn_exp2f(z - mb) : 0.f;
+    m_run = mn;
+    l_run = l_run * al + (hi == 0 ? p : 0.f);
+#pragma unroll
+    for (int d = 0; d < NO; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int dim = 32 * d + 8 * (r >> 2) + 4 * hi + (r & 3);
+        acc[d][r] *= al;
+        if (has) acc[d][r] += p * kv8_elem<BF>(A.own_v, (int64_t)oo * A.ov_row + (int64_t)h * A.ov_head + dim);
+      }
+  }
+  const float l_all = l_run + kv8_swap32(l_run);
+  auto put = [&](int d, int r, float a, float b, float e, float f) {   // four dims of the lane's column
+    const int64_t to = (int64_t)row * A.out_row + (int64_t)head * A.out_head + 32 * d + 8 * (r >> 2) + 4 * hi;
+    if constexpr (BF) *(u32x2_t*)((uint16_t*)A.out + to) = u32x2_t{kv8_pk(a, b), kv8_pk(e, f)};
+    else *(float4*)((float*)A.out + to) = make_float4(a, b, e, f);
+  };
+  if (w.splits == 1) {
+    if (!live) return;
+    const float li = l_all != 0.f ? 1.f / l_all : 0.f;
+#pragma unroll
+    for (int d = 0; d < NO; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        put(d, r, l_all != 0.f ? acc[d][r] * li : 0.f, l_all != 0.f ? acc[d][r + 1] * li : 0.f,
+            l_all != 0.f ? acc[d][r + 2] * li : 0.f, l_all != 0.f ? acc[d][r + 3] * li : 0.f);
+    return;
+  }
+  const int pf = kv8_part_floats(A.pcols, HD);
+  float* part = A.part + ((int64_t)w.slot * A.kv.H + h) * pf;
+  const int64_t pstep = (int64_t)A.kv.H * pf;
+  const int col = 32 * wv + n;
+  if (live) {
+    float* p = part + (int64_t)w.split * pstep;
+#pragma unroll
+    for (int d = 0; d < NO; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st_agent(p + col * HD + 32 * d + 8 * (r >> 2) + 4 * hi + (r & 3), acc[d][r]);
+    if (hi == 0) {
+      st_agent(p + A.pcols * HD + 2 * col, m_run);
+      st_agent(p + A.pcols * HD + 2 * col + 1, l_all);
+    }
+  }
+  if (!arrive_last(A.cnt + w.unit * A.kv.H + h, w.splits, &S.last)) return;
+  // join: two threads per column
+  const int jc = tid >> 1, half = tid & 1, jcol = c0 + jc;
+  if (jcol >= w.cols) return;
+  float M = -INFINITY, l = 0.f;
+  for (int x = 0; x < w.splits; ++x) M = fmaxf(M, ld_agent(part + (int64_t)x * pstep + A.pcols * HD + 2 * jc));
+  for (int x = 0; x < w.splits; ++x) {
+    const float* p = part + (int64_t)x * pstep + A.pcols * HD + 2 * jc;
+    const float lx = ld_agent(p + 1), y = kv8_weight(ld_agent(p), lx, M);
+    if (lx != 0.f) l += y * lx;
+  }
+  const int jrow = w.r0 + jcol / A.group, jhead = h * A.group + jcol % A.group;
+  for (int d0 = half * (HD / 2); d0 < (half + 1) * (HD / 2); d0 += 16) {
+    float a[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) a[i] = 0.f;
+    for (int x = 0; x < w.splits; ++x) {
+      const float* p = part + (int64_t)x * pstep;
+      const float lx = ld_agent(p + A.pcols * HD + 2 * jc + 1), y = kv8_weight(ld_agent(p + A.pcols * HD + 2 * jc), lx, M);
+      if (lx == 0.f) continue;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) a[i] += y * ld_agent(p + jc * HD + d0 + i);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) kv8_emit<BF>(A, jrow, jhead, d0 + i, kv8_over(a[i], l));
+  }
+}
+
+}  // namespace m2r2
