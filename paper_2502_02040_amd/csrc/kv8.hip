@@ -102,7 +102,7 @@ Cut cut(const m2r2_kv8* kv, int n_seqs, int n_rows, int n_heads) {
   c.many = cols > (long long)kFewMost * std::max(1, n_seqs);
   c.cols = c.many ? kManyCols : kFewCols;
   c.target = c.many ? 512 : 1024;
-  c.pcols = (int)std::min<long long>(c.cols, std::max<long long>(1, cols));
+  c.pcols = c.many ? kManyCols : (int)std::min<long long>(kFewCols, std::max<long long>(1, cols));
   const long long tiles = std::min<long long>(n_seqs, n_rows) + cols / c.cols;   // at most: ceil(a) <= a + 1 where a > 0
   const long long cap = (long long)kv->max_blocks_per_seq * kv->block_size;
   const long long most = tiles * std::min<long long>(kKv8MaxSplits, (cap + kKv8MinTokens - 1) / kKv8MinTokens);

@@ -160,7 +160,8 @@ __device__ __forceinline__ bool kv8_pick(const Kv8AttnArgs& A, int entry, bool r
       w.len = __shfl(len, l);
       w.splits = __shfl(splits, l);
       const int j = entry - before - __shfl(upto - mine, l), pl = __shfl(p, l);
-      w.tile = j / w.splits;
+      // (the last tile first: of a causal sequence it sees the most)
+      w.tile = __shfl(tiles, l) - 1 - j / w.splits;
       w.split = j % w.splits;
       w.t0 = min(w.len, w.split * pl);
       w.t1 = min(w.len, w.t0 + pl);
@@ -237,6 +238,16 @@ __device__ __forceinline__ void kv8_row(const void* p, int64_t at, float (&x)[N]
       }
     }
   }
+}
+
+// Two floats at once, as st_agent and ld_agent (8-byte aligned).
+__device__ __forceinline__ void st_agent2(float* p, float a, float b) {
+  const uint64_t v = __float_as_uint(a) | (uint64_t)__float_as_uint(b) << 32;
+  __hip_atomic_store((uint64_t*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 ld_agent2(const float* p) {
+  const uint64_t v = __hip_atomic_load((uint64_t*)const_cast<float*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
 }
 
 // Sum of an unnormalised result over its weight; nothing seen: zero.

@@ -31,9 +31,10 @@ struct Kv8ManyLds {
   static constexpr int VP = kManyTile + 8;
   uint16_t k[2][kManyTile * KP];              // [position][dim]
   uint16_t v[2][HD * VP];                     // [dim][position]
-  // of a tile (four in turn): positions outside the pool; whether a value is NaN that not all columns see
-  unsigned long long gap[4];
-  int odd[4];
+  // of a tile (four in turn): positions outside the pool; positions with NaN
+  // values, of a tile that not all columns see whole, and which dims' they are
+  unsigned long long gap[4], odd[4];
+  uint8_t nan[2][kManyTile][HD / 8];
   int last;
 };
 
@@ -102,22 +103,34 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
     float ks, vs;
     bool kok, vok;   // the place exists
   };
-  auto fetch = [&](int tt, Raw& r) {
+  // block ids of a tile, requested a tile before its codes
+  struct Ids {
+    int k, v;
+  };
+  auto slot = [&](int tp, int& in) {   // logical block of a position (the last one where the table ends)
+    const uint32_t lb = (uint32_t)(((uint64_t)((uint32_t)tp >> 4) * A.bs_magic) >> 31);
+    in = tp - (int)lb * A.kv.bs;
+    return min((int)lb, A.kv.mbps - 1);
+  };
+  const int* bt = A.kv.bt + (int64_t)w.s * A.kv.mbps;
+  auto ask = [&](int tt) {
     const int t = w.t0 + tt * kManyTile;
-    auto place = [&](int tp, int& rw, bool& ok) {   // per lane
+    int in;
+    return Ids{bt[slot(t + kt, in)], bt[slot(t + vt, in)]};
+  };
+  auto fetch = [&](int tt, const Ids& id, Raw& r) {
+    const int t = w.t0 + tt * kManyTile;
+    auto place = [&](int blk, int tp, int& rw, bool& ok) {
       int in;
-      const uint32_t G = (uint32_t)tp >> 4;
-      const uint32_t lb = (uint32_t)(((uint64_t)G * A.bs_magic) >> 31);
-      in = tp - (int)lb * A.kv.bs;
-      const int blk = A.kv.bt[(int64_t)w.s * A.kv.mbps + min((int)lb, A.kv.mbps - 1)];
-      ok = blk >= 0 && blk < A.kv.nb;
-      if (!ok && tp < t1) kv8_error(A.err, KV8_ERR_BLOCK);
+      slot(tp, in);
+      ok = (uint32_t)blk < (uint32_t)A.kv.nb;
+      if (!ok && tp < t1 && tt < ntile) kv8_error(A.err, KV8_ERR_BLOCK);
       const int page = (ok ? blk : 0) * A.kv.H + h;
       rw = page * A.kv.bs + in;
       return page;
     };
     int rk, rv;
-    const int pk = place(t + kt, rk, r.kok), pv = place(t + vt, rv, r.vok);
+    const int pk = place(id.k, t + kt, rk, r.kok), pv = place(id.v, t + vt, rv, r.vok);
     r.ks = A.kv.ks[pk];
     r.vs = A.kv.vs[pv];
     const uint8_t* kp = A.kv.k + (int64_t)rk * HD + kd;
@@ -142,16 +155,21 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
     }
     if (vd < HD) {
       if (t + kManyTile > least_all || !r.vok) {
-        // what no column sees is zero; NaN that some see and some do not is looked for by the waves
-        bool odd = false;
+        // what no column sees is zero in the products, and so is NaN, which must
+        // not reach the columns that do not see it
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const bool there = t + vt + x < t1 && r.vok;
-          r.v[x][0] = there ? r.v[x][0] : 0u;
-          r.v[x][1] = there ? r.v[x][1] : 0u;
-          odd |= (kv8_nan_bytes(r.v[x][0]) | kv8_nan_bytes(r.v[x][1])) != 0u;
+          uint32_t bits = 0;
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            const uint32_t nan = there ? kv8_nan_bytes(r.v[x][z]) : 0u;
+            r.v[x][z] = there ? r.v[x][z] & ~nan : 0u;
+            bits |= ((nan & 1) | (nan >> 7 & 2) | (nan >> 14 & 4) | (nan >> 21 & 8)) << (4 * z);
+          }
+          S.nan[buf][vt + x][vd / 8] = bits;
+          if (bits) atomicOr(&S.odd[tt & 3], 1ull << (vt + x));
         }
-        if (odd) S.odd[tt & 3] = 1;
       }
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
@@ -193,10 +211,13 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
   }
   __syncthreads();
   Raw ra;
+  Ids id{0, 0};
   if (ntile > 0) {
-    fetch(0, ra);
+    const Ids i0 = ask(0), i1 = ask(1);
+    fetch(0, i0, ra);
     stage(0, ra, 0);
-    if (ntile > 1) fetch(1, ra);
+    fetch(1, i1, ra);   // (beyond the last tile: some position's block, staged nowhere)
+    id = ask(2);
   }
   __syncthreads();
   // row m of a product is this position of its 32
@@ -263,49 +284,35 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
 #pragma unroll
           for (int r = 0; r < 16; ++r) acc[d][r] *= al;
       }
-      if (!full && S.odd[tt & 3]) {
-        // NaN values reach only the columns that see them
-        const int lim = min(sees, t1) - t0 - 8 * hi;
-#pragma unroll 1
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
         for (int d = 0; d < NO; ++d) {
-          f32x16_t o = acc[d], bad;
+          const u32x4_t v = *(const u32x4_t*)&S.v[buf][(32 * d + n) * VP + 16 * u + 8 * hi];
 #pragma unroll
-          for (int r = 0; r < 16; ++r) bad[r] = 0.f;
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            u32x4_t v = *(const u32x4_t*)&S.v[buf][(32 * d + n) * VP + 16 * u + 8 * hi], one, seen;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const bool n0 = (v[i] & 0x7fffu) > 0x7f80u, n1 = ((v[i] >> 16) & 0x7fffu) > 0x7f80u;
-              one[i] = (n0 ? 0x3f80u : 0u) | (n1 ? 0x3f800000u : 0u);
-              v[i] &= (n0 ? 0u : 0xffffu) | (n1 ? 0u : 0xffff0000u);
-              seen[i] = (16 * u + 2 * i < lim ? 0x3f80u : 0u) | (16 * u + 2 * i + 1 < lim ? 0x3f800000u : 0u);
-            }
-            bad = kv8_mma32(one, seen, bad);
-#pragma unroll
-            for (int p = PN - 1; p >= 0; --p) o = kv8_mma32(v, pb[u][p], o);
-          }
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[r] = bad[r] > 0.f ? __uint_as_float(0x7fc00000u) : o[r];
-#pragma unroll
-          for (int e = 0; e < NO; ++e)
-            if (e == d) acc[e] = o;
+          for (int p = PN - 1; p >= 0; --p) acc[d] = kv8_mma32(v, pb[u][p], acc[d]);
         }
-      } else {
+      // NaN values, which the products took as zero, for the columns that see them
+      for (unsigned long long odd = S.odd[tt & 3]; odd; odd &= odd - 1) {
+        const int p = __ffsll(odd) - 1;
+        if (t0 + p < min(sees, t1)) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+          for (int d = 0; d < NO; ++d)
 #pragma unroll
-          for (int d = 0; d < NO; ++d) {
-            const u32x4_t v = *(const u32x4_t*)&S.v[buf][(32 * d + n) * VP + 16 * u + 8 * hi];
+            for (int r = 0; r < 16; r += 4) {
+              const uint32_t bits = S.nan[buf][p][4 * d + (r >> 2)] >> (4 * hi);
 #pragma unroll
-            for (int p = PN - 1; p >= 0; --p) acc[d] = kv8_mma32(v, pb[u][p], acc[d]);
-          }
+              for (int i = 0; i < 4; ++i)
+                if ((bits >> i) & 1) acc[d][r + i] = __uint_as_float(0x7fc00000u);
+            }
+        }
       }
     }
     if (tt + 1 < ntile) {
       // (the other buffer's readers passed the last barrier)
       stage(tt + 1, ra, buf ^ 1);
-      if (tt + 2 < ntile) fetch(tt + 2, ra);
+      if (tt + 2 < ntile) fetch(tt + 2, id, ra);
+      id = ask(tt + 3);
       __syncthreads();
     }
   }
@@ -355,47 +362,56 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
             l_all != 0.f ? acc[d][r + 2] * li : 0.f, l_all != 0.f ? acc[d][r + 3] * li : 0.f);
     return;
   }
-  const int pf = kv8_part_floats(A.pcols, HD);
+  // Partial results as the lanes hold them: of each wave the accumulators, 16
+  // bytes a lane, then the maximum and sum of its columns.
+  const int pf = kv8_part_floats(kManyCols, HD);
   float* part = A.part + ((int64_t)w.slot * A.kv.H + h) * pf;
   const int64_t pstep = (int64_t)A.kv.H * pf;
-  const int col = 32 * wv + n;
-  if (live) {
+  const int mine = wv * 32 * HD, ml = kManyCols * HD + 2 * (32 * wv + n);
+  {
     float* p = part + (int64_t)w.split * pstep;
 #pragma unroll
     for (int d = 0; d < NO; ++d)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) st_agent(p + col * HD + 32 * d + 8 * (r >> 2) + 4 * hi + (r & 3), acc[d][r]);
-    if (hi == 0) {
-      st_agent(p + A.pcols * HD + 2 * col, m_run);
-      st_agent(p + A.pcols * HD + 2 * col + 1, l_all);
-    }
+      for (int r = 0; r < 16; r += 4) {
+        float* o = p + mine + ((4 * d + (r >> 2)) * 64 + lane) * 4;
+        st_agent2(o, acc[d][r], acc[d][r + 1]);
+        st_agent2(o + 2, acc[d][r + 2], acc[d][r + 3]);
+      }
+    if (hi == 0) st_agent2(p + ml, m_run, l_all);
   }
   if (!arrive_last(A.cnt + w.unit * A.kv.H + h, w.splits, &S.last)) return;
-  // join: two threads per column
-  const int jc = tid >> 1, half = tid & 1, jcol = c0 + jc;
-  if (jcol >= w.cols) return;
   float M = -INFINITY, l = 0.f;
-  for (int x = 0; x < w.splits; ++x) M = fmaxf(M, ld_agent(part + (int64_t)x * pstep + A.pcols * HD + 2 * jc));
+  for (int x = 0; x < w.splits; ++x) M = fmaxf(M, ld_agent(part + (int64_t)x * pstep + ml));
+#pragma unroll
+  for (int d = 0; d < NO; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
   for (int x = 0; x < w.splits; ++x) {
-    const float* p = part + (int64_t)x * pstep + A.pcols * HD + 2 * jc;
-    const float lx = ld_agent(p + 1), y = kv8_weight(ld_agent(p), lx, M);
-    if (lx != 0.f) l += y * lx;
-  }
-  const int jrow = w.r0 + jcol / A.group, jhead = h * A.group + jcol % A.group;
-  for (int d0 = half * (HD / 2); d0 < (half + 1) * (HD / 2); d0 += 16) {
-    float a[16];
+    const float* p = part + (int64_t)x * pstep;
+    const float lx = ld_agent(p + ml + 1), y = kv8_weight(ld_agent(p + ml), lx, M);
+    float2 v[NO][8];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) a[i] = 0.f;
-    for (int x = 0; x < w.splits; ++x) {
-      const float* p = part + (int64_t)x * pstep;
-      const float lx = ld_agent(p + A.pcols * HD + 2 * jc + 1), y = kv8_weight(ld_agent(p + A.pcols * HD + 2 * jc), lx, M);
-      if (lx == 0.f) continue;
+    for (int d = 0; d < NO; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) a[i] += y * ld_agent(p + jc * HD + d0 + i);
+      for (int r = 0; r < 8; ++r) v[d][r] = ld_agent2(p + mine + ((4 * d + (r >> 1)) * 64 + lane) * 4 + 2 * (r & 1));
+    if (lx != 0.f) {
+      l += y * lx;
+#pragma unroll
+      for (int d = 0; d < NO; ++d)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          acc[d][2 * r] += y * v[d][r].x;
+          acc[d][2 * r + 1] += y * v[d][r].y;
+        }
     }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) kv8_emit<BF>(A, jrow, jhead, d0 + i, kv8_over(a[i], l));
   }
+  if (!live) return;
+#pragma unroll
+  for (int d = 0; d < NO; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4)
+      put(d, r, kv8_over(acc[d][r], l), kv8_over(acc[d][r + 1], l), kv8_over(acc[d][r + 2], l), kv8_over(acc[d][r + 3], l));
 }
 
 }  // namespace m2r2
