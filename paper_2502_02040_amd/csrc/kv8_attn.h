@@ -93,14 +93,29 @@ __device__ __forceinline__ uint32_t kv8_nan_bytes(uint32_t w) {
   return (t >> 7) * 0xffu;
 }
 
+// Integer steps across lanes without LDS: DPP within rows of 16 lanes and from
+// row to row.
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ int kv8_dpp0(int v) {   // 0 where there is no source
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
 __device__ __forceinline__ int kv8_wave_scan(int v) {   // inclusive sum
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(v, d);
-    v += lane >= d ? o : 0;
-  }
-  return v;
+  v += kv8_dpp0<0x111>(v);
+  v += kv8_dpp0<0x112>(v);
+  v += kv8_dpp0<0x114>(v);
+  v += kv8_dpp0<0x118>(v);
+  v += kv8_dpp0<0x142, 0xa>(v);   // the last lane of the row before
+  return v + kv8_dpp0<0x143, 0xc>(v);
+}
+template <int CTRL>
+__device__ __forceinline__ int kv8_dpp(int v) {
+  return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false);
+}
+__device__ __forceinline__ int kv8_row_max(int v) {   // over 16 lanes, in all of them
+  v = max(v, kv8_dpp<kDppQuadXor1>(v));
+  v = max(v, kv8_dpp<kDppQuadXor2>(v));
+  v = max(v, kv8_dpp<kDppRowHalfMirror>(v));
+  return max(v, kv8_dpp<kDppRowMirror>(v));
 }
 
 // One workgroup's piece of a call.
@@ -127,26 +142,31 @@ __device__ __forceinline__ void kv8_seq(const Kv8AttnArgs& A, int s, bool report
 // Piece `entry` of the launch, the same in every wave.  Splits are as long as
 // an even share of all tiles' positions, so that sequences of very different
 // lengths keep every compute unit busy to the end.
+__device__ __forceinline__ int kv8_split_len(const Kv8AttnArgs& A, float sum) {
+  // (a little more than the share: the float sum may be that much too small)
+  const float share = sum * (float)A.kv.H / (float)A.target * 1.002f;
+  return max(kKv8MinTokens, ((int)min(share, 1e9f) / 64 + 1) * 64);
+}
 template <int TC>
 __device__ __forceinline__ bool kv8_pick(const Kv8AttnArgs& A, int entry, bool report, Kv8Work& w) {
   const int lane = threadIdx.x & 63;
   float sum = 0.f;
+  int r0 = 0, cols = 0, len = 0, tiles = 0;
   for (int c = 0; c < A.n_seqs; c += 64) {
-    int r0, cols, len;
-    kv8_seq<TC>(A, min(c + lane, A.n_seqs - 1), report && c + lane < A.n_seqs, r0, cols, len);
-    if (c + lane < A.n_seqs) sum += (float)((cols + TC - 1) / TC) * (float)len;
+    const bool mine = c + lane < A.n_seqs;
+    kv8_seq<TC>(A, mine ? c + lane : A.n_seqs - 1, report && mine, r0, cols, len);
+    tiles = mine ? (cols + TC - 1) / TC : 0;
+    sum += (float)tiles * (float)len;
   }
-  sum = wave_sum(sum);
-  // (a little more than the share: the float sum may be that much too small)
-  const float share = sum * (float)A.kv.H / (float)A.target * 1.002f;
-  const int per = max(kKv8MinTokens, ((int)min(share, 1e9f) / 64 + 1) * 64);
+  const int per = kv8_split_len(A, wave_sum(sum));
   int before = 0, slots = 0, units = 0;
   w.s = -1;
   for (int c = 0; c < A.n_seqs; c += 64) {
-    const int s = min(c + lane, A.n_seqs - 1);
-    int r0, cols, len;
-    kv8_seq<TC>(A, s, false, r0, cols, len);
-    const int tiles = c + lane < A.n_seqs ? (cols + TC - 1) / TC : 0;
+    if (A.n_seqs > 64) {
+      const bool mine = c + lane < A.n_seqs;
+      kv8_seq<TC>(A, mine ? c + lane : A.n_seqs - 1, false, r0, cols, len);
+      tiles = mine ? (cols + TC - 1) / TC : 0;
+    }
     const int p = max(per, ((len + kKv8MaxSplits - 1) / kKv8MaxSplits + 63) / 64 * 64);
     const int splits = max(1, (len + p - 1) / p);
     const int mine = tiles * splits, ms = splits > 1 ? mine : 0, mu = splits > 1 ? tiles : 0;
@@ -154,23 +174,24 @@ __device__ __forceinline__ bool kv8_pick(const Kv8AttnArgs& A, int entry, bool r
     const uint64_t hit = __ballot(entry >= before + upto - mine && entry < before + upto);
     if (hit) {
       const int l = __ffsll((unsigned long long)hit) - 1;
+      auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
       w.s = c + l;
-      w.r0 = __shfl(r0, l);
-      w.cols = __shfl(cols, l);
-      w.len = __shfl(len, l);
-      w.splits = __shfl(splits, l);
-      const int j = entry - before - __shfl(upto - mine, l), pl = __shfl(p, l);
+      w.r0 = of(r0);
+      w.cols = of(cols);
+      w.len = of(len);
+      w.splits = of(splits);
+      const int j = entry - before - of(upto - mine), pl = of(p);
       // (the last tile first: of a causal sequence it sees the most)
-      w.tile = __shfl(tiles, l) - 1 - j / w.splits;
+      w.tile = of(tiles) - 1 - j / w.splits;
       w.split = j % w.splits;
       w.t0 = min(w.len, w.split * pl);
       w.t1 = min(w.len, w.t0 + pl);
-      w.slot = slots + __shfl(us - ms, l) + w.tile * w.splits;
-      w.unit = units + __shfl(uu - mu, l) + w.tile;
+      w.slot = slots + of(us - ms) + w.tile * w.splits;
+      w.unit = units + of(uu - mu) + w.tile;
     }
-    before += __shfl(upto, 63);
-    slots += __shfl(us, 63);
-    units += __shfl(uu, 63);
+    before += __builtin_amdgcn_readlane(upto, 63);
+    slots += __builtin_amdgcn_readlane(us, 63);
+    units += __builtin_amdgcn_readlane(uu, 63);
   }
   // row starts that overlap can ask for more than the grid holds: nothing is done then
   if (before > A.entries) {

@@ -96,6 +96,12 @@ struct Kv8Few {
     for (int i = 0; i < 2; ++i) p.p[i] = kv8_place(A, h, b.b[i], b.in[i]);
     return p;
   }
+  // Scalar loads return in any order: a wait for one waits for all.  This is the
+  // one wait of a tile, for what the tile before requested, ahead of its own requests.
+  static __device__ __forceinline__ void arrived(const Blocks& b, const Places& p) {
+    asm volatile("" ::"s"(b.b[0]), "s"(b.b[1]), "s"(p.p[0].ks), "s"(p.p[0].vs), "s"(p.p[1].ks), "s"(p.p[1].vs));
+    __builtin_amdgcn_sched_barrier(0);
+  }
   static __device__ __forceinline__ void load(const Kv8AttnArgs& A, const Places& p, Tile& t) {
     const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     const int rk = max((m >> 3) ? p.p[1].row : p.p[0].row, 0), rv = max((g >> 1) ? p.p[1].row : p.p[0].row, 0);
@@ -240,41 +246,34 @@ struct Kv8Few {
 __host__ __device__ constexpr int kv8_part_floats(int cols, int hd) { return cols * (hd + 2); }
 
 template <int BF>
-__device__ __forceinline__ void kv8_emit(const Kv8AttnArgs& A, int row, int head, int d, float v) {
+__device__ __forceinline__ void kv8_emit2(const Kv8AttnArgs& A, int row, int head, int d, float a, float b) {
   const int64_t to = (int64_t)row * A.out_row + (int64_t)head * A.out_head + d;
-  if constexpr (BF) ((__bf16*)A.out)[to] = (__bf16)v;
-  else ((float*)A.out)[to] = v;
+  if constexpr (BF) *(uint32_t*)((uint16_t*)A.out + to) = kv8_pk(a, b);
+  else *(float2*)((float*)A.out + to) = make_float2(a, b);
 }
 
 template <int BF, int HD>
 __global__ __launch_bounds__(kFewThreads, 2) void k8_few(Kv8AttnArgs A) {
-  using F = Kv8Few<BF, HD>;
   constexpr int OD = HD / 16;   // dims of a thread of the own keys
   __shared__ __attribute__((aligned(16))) float acc_s[kFewWaves][kFewCols][HD];
   __shared__ float m_s[kFewWaves][kFewCols], l_s[kFewWaves][kFewCols];
   __shared__ float ov_s[kFewCols][HD], oz_s[kFewCols];   // own values and scores (first split)
-  __shared__ float mw[kFewCols][kKv8MaxSplits], lw[kFewCols][kKv8MaxSplits], li_s[kFewCols];
+  __shared__ float mw[kFewCols][kKv8MaxSplits], li_s[kFewCols];
   __shared__ int last_s;
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = blockIdx.x % A.kv.H, entry = blockIdx.x / A.kv.H;
   Kv8Work w;
   if (!kv8_pick<kFewCols>(A, entry, blockIdx.x == 0 && wv == 0, w)) return;
-  // (uniform: the loads that depend on them are scalar)
-  w.s = __builtin_amdgcn_readfirstlane(w.s);
-  w.t0 = __builtin_amdgcn_readfirstlane(w.t0);
-  w.t1 = __builtin_amdgcn_readfirstlane(w.t1);
   const int c0 = w.tile * kFewCols, live = min(kFewCols, w.cols - c0);
   const int q = lane & 15, c = c0 + q;
+  using F = Kv8Few<BF, HD>;
+  int tt = wv;
+  const typename F::Blocks b0 = F::blocks(A, w.s, w.t0 + tt * kFewTile);   // (needed or not)
   const int sees = kv8_sees(A, w, c);
   // positions that any, and that every live column sees
   int most = sees, least = q < live ? sees : 1 << 30;
-#pragma unroll
-  for (int d = 1; d < 16; d <<= 1) {
-    most = max(most, __shfl_xor(most, d));
-    least = min(least, __shfl_xor(least, d));
-  }
-  most = __builtin_amdgcn_readfirstlane(most);
-  least = __builtin_amdgcn_readfirstlane(least);
+  most = __builtin_amdgcn_readfirstlane(kv8_row_max(most));
+  least = -__builtin_amdgcn_readfirstlane(kv8_row_max(-least));
   const int t1 = min(w.t1, most);
   const int ntile = t1 > w.t0 ? (t1 - w.t0 + kFewTile - 1) / kFewTile : 0;
   const float sc = A.scale * kLog2e;
@@ -283,9 +282,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void k8_few(Kv8AttnArgs A) {
   typename F::Places pa, pb;
   typename F::Blocks bn;
   auto at = [&](int tt) { return w.t0 + min(tt, max(ntile - 1, 0)) * kFewTile; };
-  int tt = wv;
   if (tt < ntile) {
-    pa = F::places(A, h, F::blocks(A, w.s, at(tt)));
+    pa = F::places(A, h, b0);
     F::load(A, pa, ta);
     bn = F::blocks(A, w.s, at(tt + kFewWaves));
   }
@@ -312,95 +310,134 @@ __global__ __launch_bounds__(kFewThreads, 2) void k8_few(Kv8AttnArgs A) {
     if (part == 0) oz_s[oc] = has ? z : -INFINITY;
   }
   f.init(A, w, h, c);
-  auto step = [&](typename F::Tile& t, const typename F::Places& p) {
-    const int t0 = w.t0 + tt * kFewTile;
-    const bool ok = p.p[0].row >= 0 && p.p[1].row >= 0;
-    if (t0 + kFewTile <= least && ok) {
-      f.template tile<true>(t, p, sc, 0, 0);
-    } else {
-      // (a group outside the pool is not seen)
-      const int g = lane >> 4;
-      const bool gone = p.p[g >> 1].row < 0;
-      const bool gap = t0 + 16 * (g >> 1) < most && gone;
-      if (gap && (lane & 15) == 0) kv8_error(A.err, KV8_ERR_BLOCK);
-      f.template tile<false>(t, p, sc, gone ? 0 : min(sees, t1) - t0, gone ? 0 : t1 - t0);
-    }
+  // Tiles that every live column sees whole; the next tile's codes are in flight
+  // meanwhile, whatever kind it is.
+  const int nfull = min(ntile, max(0, (least - w.t0) / kFewTile));
+  auto there = [](const typename F::Places& p) { return p.p[0].row >= 0 && p.p[1].row >= 0; };
+  auto next = [&](const typename F::Places& have, typename F::Tile& t, typename F::Places& p) {
+    F::arrived(bn, have);
+    p = F::places(A, h, bn);
+    bn = F::blocks(A, w.s, at(tt + 2 * kFewWaves));
+    if (tt + kFewWaves < ntile) F::load(A, p, t);
+    __builtin_amdgcn_sched_barrier(0);
   };
+  while (tt < nfull && there(pa)) {
+    next(pa, tb, pb);
+    f.template tile<true>(ta, pa, sc, 0, 0);
+    tt += kFewWaves;
+    if (tt >= nfull || !there(pb)) {
+      ta = tb;
+      pa = pb;
+      break;
+    }
+    next(pb, ta, pa);
+    f.template tile<true>(tb, pb, sc, 0, 0);
+    tt += kFewWaves;
+  }
+  // the others: at the end of what a column sees, or with positions outside the
+  // pool, which are not seen
   while (tt < ntile) {
-    pb = F::places(A, h, bn);
-    if (tt + kFewWaves < ntile) F::load(A, pb, tb);
-    bn = F::blocks(A, w.s, at(tt + 2 * kFewWaves));
-    step(ta, pa);
+    const int t0 = w.t0 + tt * kFewTile, g = lane >> 4;
+    const bool gone = (g >> 1 ? pa.p[1].row : pa.p[0].row) < 0;
+    if (gone && t0 + 16 * (g >> 1) < most && (lane & 15) == 0) kv8_error(A.err, KV8_ERR_BLOCK);
+    f.template tile<false>(ta, pa, sc, gone ? 0 : min(sees, t1) - t0, gone ? 0 : t1 - t0);
     tt += kFewWaves;
-    if (tt >= ntile) break;
-    pa = F::places(A, h, bn);
-    if (tt + kFewWaves < ntile) F::load(A, pa, ta);
-    bn = F::blocks(A, w.s, at(tt + 2 * kFewWaves));
-    step(tb, pb);
-    tt += kFewWaves;
+    if (tt < ntile) {
+      pa = F::places(A, h, bn);
+      F::load(A, pa, ta);
+      bn = F::blocks(A, w.s, at(tt + kFewWaves));
+    }
   }
   f.store(&m_s[wv][q], &l_s[wv][q], acc_s[wv][q]);
   __syncthreads();
   // ---- the waves' results, and the own key's, combined -------------------------
   float* part = A.part + ((int64_t)w.slot * A.kv.H + h) * kv8_part_floats(A.pcols, HD);
   const int64_t pstep = (int64_t)A.kv.H * kv8_part_floats(A.pcols, HD);
-  for (int e = tid; e < live * HD; e += kFewThreads) {
+  for (int e = 2 * tid; e < live * HD; e += 2 * kFewThreads) {
     const int i = e / HD, d = e % HD;
     const float oz = own ? oz_s[i] : -INFINITY;
     float M = oz;
 #pragma unroll
     for (int x = 0; x < kFewWaves; ++x) M = fmaxf(M, m_s[x][i]);
     float l = oz != -INFINITY ? __builtin_amdgcn_exp2f(oz - M) : 0.f;
-    float a = l != 0.f ? l * ov_s[i][d] : 0.f;
+    float a = 0.f, b = 0.f;
+    if (l != 0.f) {
+      a = l * ov_s[i][d];
+      b = l * ov_s[i][d + 1];
+    }
 #pragma unroll
     for (int x = 0; x < kFewWaves; ++x) {
       const float y = kv8_weight(m_s[x][i], l_s[x][i], M);
       if (l_s[x][i] != 0.f) {
-        a += y * acc_s[x][i][d];
+        const float2 o = *(const float2*)&acc_s[x][i][d];
+        a += y * o.x;
+        b += y * o.y;
         l += y * l_s[x][i];
       }
     }
     if (w.splits == 1) {
-      kv8_emit<BF>(A, w.r0 + (c0 + i) / A.group, h * A.group + (c0 + i) % A.group, d, kv8_over(a, l));
+      kv8_emit2<BF>(A, w.r0 + (c0 + i) / A.group, h * A.group + (c0 + i) % A.group, d, kv8_over(a, l), kv8_over(b, l));
     } else {
       float* p = part + (int64_t)w.split * pstep;
-      st_agent(p + e, a);
-      if (d == 0) {
-        st_agent(p + A.pcols * HD + 2 * i, M);
-        st_agent(p + A.pcols * HD + 2 * i + 1, l);
-      }
+      st_agent2(p + e, a, b);
+      if (d == 0) st_agent2(p + A.pcols * HD + 2 * i, M, l);
     }
   }
   if (w.splits == 1) return;
   // ---- the last split to arrive joins them ---------------------------------------
   if (!arrive_last(A.cnt + w.unit * A.kv.H + h, w.splits, &last_s)) return;
-  for (int e = tid; e < live * w.splits; e += kFewThreads) {
-    const int i = e / w.splits, x = e % w.splits;
-    const float* p = part + (int64_t)x * pstep + A.pcols * HD + 2 * i;
-    mw[i][x] = ld_agent(p);
-    lw[i][x] = ld_agent(p + 1);
+  // Pairs of dims; where a column or two leave threads over, groups of threads
+  // take every so-manieth split each.  The first loads do not wait for the weights.
+  constexpr int UN = 16;
+  const int pairs = live * (HD / 2);
+  const int groups = pairs <= kFewThreads / 4 ? 4 : pairs <= kFewThreads / 2 ? 2 : 1;
+  const int width = kFewThreads / groups;
+  const int grp = tid / width, e0 = tid % width;
+  auto at_split = [&](int x) { return part + (int64_t)min(x, w.splits - 1) * pstep; };
+  float2 v[UN];
+#pragma unroll
+  for (int u = 0; u < UN; ++u) v[u] = ld_agent2(at_split(grp + u * groups) + 2 * min(e0, pairs - 1));
+  for (int i = wv; i < live; i += kFewWaves) {   // a wave per column, a lane per split
+    const float2 ml = ld_agent2(at_split(lane) + A.pcols * HD + 2 * i);
+    const float m = lane < w.splits ? ml.x : -INFINITY, l = lane < w.splits ? ml.y : 0.f;
+    const float y = kv8_weight(m, l, wave_max(m));
+    mw[i][lane] = y;
+    const float s = wave_sum(l != 0.f ? y * l : 0.f);
+    if (lane == 0) li_s[i] = s;
   }
   __syncthreads();
-  if (tid < live) {
-    float M = -INFINITY, l = 0.f;
-    for (int x = 0; x < w.splits; ++x) M = fmaxf(M, mw[tid][x]);
-    for (int x = 0; x < w.splits; ++x) {
-      const float y = kv8_weight(mw[tid][x], lw[tid][x], M);
-      mw[tid][x] = y;
-      if (lw[tid][x] != 0.f) l += y * lw[tid][x];
+  for (int e = e0; e - e0 < pairs; e += width) {
+    const int ee = min(e, pairs - 1), i = 2 * ee / HD;
+    float a = 0.f, b = 0.f;
+    for (int x = grp; x < w.splits; x += UN * groups) {
+      if (x != grp || e != e0) {
+#pragma unroll
+        for (int u = 0; u < UN; ++u) v[u] = ld_agent2(at_split(x + u * groups) + 2 * ee);
+      }
+#pragma unroll
+      for (int u = 0; u < UN; ++u) {
+        // (past the last split: weight zero)
+        const float y = x + u * groups < w.splits ? mw[i][x + u * groups] : 0.f;
+        a += y != 0.f ? y * v[u].x : 0.f;
+        b += y != 0.f ? y * v[u].y : 0.f;
+      }
     }
-    li_s[tid] = l;
-  }
-  __syncthreads();
-  for (int e = tid; e < live * HD; e += kFewThreads) {
-    const int i = e / HD, d = e % HD;
-    float a = 0.f;
-#pragma unroll 16
-    for (int x = 0; x < w.splits; ++x) {
-      const float v = ld_agent(part + (int64_t)x * pstep + e);
-      if (lw[i][x] != 0.f) a += mw[i][x] * v;
+    if (groups > 1) {   // (one turn of the loop: at most `width` pairs)
+      float2* red = (float2*)&acc_s[0][0][0];
+      if (e < pairs) red[grp * width + e] = make_float2(a, b);
+      __syncthreads();
+      if (grp == 0 && e < pairs) {
+        a = b = 0.f;
+        for (int g2 = 0; g2 < groups; ++g2) {
+          a += red[g2 * width + e].x;
+          b += red[g2 * width + e].y;
+        }
+      }
     }
-    kv8_emit<BF>(A, w.r0 + (c0 + i) / A.group, h * A.group + (c0 + i) % A.group, d, kv8_over(a, li_s[i]));
+    if (grp == 0 && e < pairs) {
+      kv8_emit2<BF>(A, w.r0 + (c0 + i) / A.group, h * A.group + (c0 + i) % A.group, 2 * e - i * HD,
+                    kv8_over(a, li_s[i]), kv8_over(b, li_s[i]));
+    }
   }
 }
 

@@ -62,9 +62,6 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
   const int h = blockIdx.x % A.kv.H, entry = blockIdx.x / A.kv.H;
   Kv8Work w;
   if (!kv8_pick<kManyCols>(A, entry, blockIdx.x == 0 && wv == 0, w)) return;
-  w.s = __builtin_amdgcn_readfirstlane(w.s);
-  w.t0 = __builtin_amdgcn_readfirstlane(w.t0);
-  w.t1 = __builtin_amdgcn_readfirstlane(w.t1);
   const int c0 = w.tile * kManyCols, c = c0 + 32 * wv + n;
   const bool live = c < w.cols;
   const int cc = min(c, w.cols - 1);
