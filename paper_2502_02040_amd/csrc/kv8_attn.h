@@ -24,11 +24,14 @@ struct Kv8AttnArgs {
   float* part;       // partial results
   int pcols;         // columns of a partial result
   int target;        // workgroups that a launch is cut into, about
+  int max_splits;    // of a tile
   int entries;       // (tile, split) pairs that the grid covers
   uint32_t bs_magic; // ceil(2^31 / (bs / 16))
 };
 
-constexpr int kKv8MaxSplits = 64;      // of a tile (the join's weights are in LDS)
+constexpr int kKv8Units = 256;         // compute units
+constexpr int kKv8FullTokens = 512;
+constexpr int kKv8MaxSplits = 64;      // of a tile: a lane each in the join
 constexpr int kKv8MinTokens = 128;     // of a split, at least: a tile of 32 for each of four waves
 constexpr int kKv8Counters = 16384;    // split tiles of a call, at most
 
@@ -140,12 +143,18 @@ __device__ __forceinline__ void kv8_seq(const Kv8AttnArgs& A, int s, bool report
 }
 
 // Piece `entry` of the launch, the same in every wave.  Splits are as long as
-// an even share of all tiles' positions, so that sequences of very different
-// lengths keep every compute unit busy to the end.
+// an even share of all tiles' positions among the workgroups that fit the chip
+// (target), so that sequences of very different lengths keep every compute unit
+// busy to the end; shorter than kKv8FullTokens only as far as every compute unit
+// gets one.  Measured (32 query heads over 8 of 128): one sequence of 16384
+// positions 17.1 us in splits of 512, 20.9 in splits of 256; four of 8192 15.9 and
+// 18.7; where the share is longer than that, a share of 768 workgroups against
+// one of 256: eight sequences of 4096 (32 heads of 96) 27.8 and 32.5.
 __device__ __forceinline__ int kv8_split_len(const Kv8AttnArgs& A, float sum) {
   // (a little more than the share: the float sum may be that much too small)
-  const float share = sum * (float)A.kv.H / (float)A.target * 1.002f;
-  return max(kKv8MinTokens, ((int)min(share, 1e9f) / 64 + 1) * 64);
+  const float all = min(sum * (float)A.kv.H * 1.002f, 1e18f);
+  const float share = max(all / (float)A.target, min(all / (float)kKv8Units, (float)kKv8FullTokens));
+  return max(kKv8MinTokens, ((int)min(share, 1e9f) + 63) / 64 * 64);
 }
 template <int TC>
 __device__ __forceinline__ bool kv8_pick(const Kv8AttnArgs& A, int entry, bool report, Kv8Work& w) {
@@ -167,7 +176,7 @@ __device__ __forceinline__ bool kv8_pick(const Kv8AttnArgs& A, int entry, bool r
       kv8_seq<TC>(A, mine ? c + lane : A.n_seqs - 1, false, r0, cols, len);
       tiles = mine ? (cols + TC - 1) / TC : 0;
     }
-    const int p = max(per, ((len + kKv8MaxSplits - 1) / kKv8MaxSplits + 63) / 64 * 64);
+    const int p = max(per, ((len + A.max_splits - 1) / A.max_splits + 63) / 64 * 64);
     const int splits = max(1, (len + p - 1) / p);
     const int mine = tiles * splits, ms = splits > 1 ? mine : 0, mu = splits > 1 ? tiles : 0;
     const int upto = kv8_wave_scan(mine), us = kv8_wave_scan(ms), uu = kv8_wave_scan(mu);

@@ -392,13 +392,19 @@ __global__ __launch_bounds__(kFewThreads, 2) void k8_few(Kv8AttnArgs A) {
   const int pairs = live * (HD / 2);
   const int groups = pairs <= kFewThreads / 4 ? 4 : pairs <= kFewThreads / 2 ? 2 : 1;
   const int width = kFewThreads / groups;
-  const int grp = tid / width, e0 = tid % width;
-  auto at_split = [&](int x) { return part + (int64_t)min(x, w.splits - 1) * pstep; };
+  const int grp = __builtin_amdgcn_readfirstlane(tid / width), e0 = tid % width;
+  auto at_split = [&](int x) { return part + (int64_t)x * pstep; };
   float2 v[UN];
+  auto request = [&](int x, int e) {   // splits x, x + groups, ...
 #pragma unroll
-  for (int u = 0; u < UN; ++u) v[u] = ld_agent2(at_split(grp + u * groups) + 2 * min(e0, pairs - 1));
+    for (int u = 0; u < UN; ++u) {
+      v[u] = make_float2(0.f, 0.f);
+      if (x + u * groups < w.splits) v[u] = ld_agent2(at_split(x + u * groups) + 2 * e);
+    }
+  };
+  request(grp, min(e0, pairs - 1));
   for (int i = wv; i < live; i += kFewWaves) {   // a wave per column, a lane per split
-    const float2 ml = ld_agent2(at_split(lane) + A.pcols * HD + 2 * i);
+    const float2 ml = ld_agent2(at_split(min(lane, w.splits - 1)) + A.pcols * HD + 2 * i);
     const float m = lane < w.splits ? ml.x : -INFINITY, l = lane < w.splits ? ml.y : 0.f;
     const float y = kv8_weight(m, l, wave_max(m));
     mw[i][lane] = y;
@@ -410,10 +416,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void k8_few(Kv8AttnArgs A) {
     const int ee = min(e, pairs - 1), i = 2 * ee / HD;
     float a = 0.f, b = 0.f;
     for (int x = grp; x < w.splits; x += UN * groups) {
-      if (x != grp || e != e0) {
-#pragma unroll
-        for (int u = 0; u < UN; ++u) v[u] = ld_agent2(at_split(x + u * groups) + 2 * ee);
-      }
+      if (x != grp || e != e0) request(x, ee);
 #pragma unroll
       for (int u = 0; u < UN; ++u) {
         // (past the last split: weight zero)
