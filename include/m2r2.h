@@ -36,7 +36,7 @@
  *    are stored in the configured weight dtype; norm gains are always float32.
  *  - KV cache: paged, slow stream only.  K and V pages are
  *    [n_layers][num_blocks][n_heads][block_size][head_dim] in the configured
- *    KV dtype; block_table is [batch][max_blocks_per_seq] int32 (physical
+ *    KV dtype (M2R2_FP8: bytes, with scales [n_layers][num_blocks][n_heads]); block_table is [batch][max_blocks_per_seq] int32 (physical
  *    block of each logical block, shared by all layers).  Positions outside a
  *    sequence's block table are not read or written (a sticky device error
  *    bit is set instead).
@@ -75,7 +75,11 @@ typedef enum {
   M2R2_E_UNSUPPORTED = -7   /* valid request the library does not implement */
 } m2r2_status;
 
-typedef enum { M2R2_F32 = 0, M2R2_BF16 = 1 } m2r2_dtype;
+typedef enum {
+  M2R2_F32 = 0,
+  M2R2_BF16 = 1,
+  M2R2_FP8 = 2   /* of the KV cache only: e4m3 codes with a scale per block and head (m2r2_kv8.h) */
+} m2r2_dtype;
 
 /* Exit handling at gates (Fig. 3 caption; Eq. 4).
  *  OFF:     no gate is evaluated; p is never re-initialised.
@@ -91,7 +95,10 @@ typedef enum { M2R2_EXIT_OFF = 0, M2R2_EXIT_OBSERVE = 1, M2R2_EXIT_EXIT = 2 } m2
 typedef struct {
   int32_t n_layers, d_model, n_heads, head_dim, ffn, vocab, rank;
   int32_t wdtype;           /* m2r2_dtype of matrices, embeddings, adapters */
-  int32_t kvdtype;          /* m2r2_dtype of the KV pages */
+  /* m2r2_dtype of the KV pages.  M2R2_FP8: dense models in the memory-bound
+   * form (M2R2_E_UNSUPPORTED otherwise); a slow row's key and value at its own
+   * position are seen as cached, a fast row's own are exact. */
+  int32_t kvdtype;
   float rms_eps;            /* RMSNorm epsilon */
   float rope_theta;         /* rotate-half RoPE base */
   /* Mixture of experts (Sec. 2.3.3); n_experts = 0 for a dense model.  Every
@@ -169,6 +176,9 @@ typedef struct {
   const int32_t* block_table_d;  /* [batch][max_blocks_per_seq] */
   int32_t* seq_lens_d;           /* [batch]: written with the number of valid cache positions */
   int32_t num_blocks, block_size, max_blocks_per_seq;
+  /* M2R2_FP8 only (not read otherwise): [n_layers][num_blocks][n_heads]; block_size is then a multiple of 16, at most 256 */
+  float* k_scales;
+  float* v_scales;
 } m2r2_kv;
 
 typedef struct {

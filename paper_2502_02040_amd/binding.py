@@ -16,7 +16,8 @@ import numpy as np
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libm2r2.so")
 
-F32, BF16 = 0, 1
+F32, BF16, FP8 = 0, 1, 2   # (FP8: of the KV cache only)
+KV_DTYPES = {"f32": F32, "bf16": BF16, "fp8": FP8}
 EXIT_OFF, EXIT_OBSERVE, EXIT_EXIT = 0, 1, 2
 MODES = {"off": EXIT_OFF, "observe": EXIT_OBSERVE, "exit": EXIT_EXIT}
 PROJ = ("q", "k", "v", "o", "g", "u", "d")
@@ -58,7 +59,8 @@ class Weights(ctypes.Structure):
 
 class KV(ctypes.Structure):
     _fields_ = [("k_pages", c_void_p), ("v_pages", c_void_p), ("block_table_d", c_void_p), ("seq_lens_d", c_void_p),
-                ("num_blocks", c_int32), ("block_size", c_int32), ("max_blocks_per_seq", c_int32)]
+                ("num_blocks", c_int32), ("block_size", c_int32), ("max_blocks_per_seq", c_int32),
+                ("k_scales", c_void_p), ("v_scales", c_void_p)]
 
 
 class Exit(ctypes.Structure):
@@ -162,7 +164,7 @@ def _stream(stream) -> int:
 def make_config(cfg, expert_slots: Optional[int] = None) -> Config:
     slots = cfg.n_experts if expert_slots is None else expert_slots
     return Config(cfg.n_layers, cfg.d_model, cfg.n_heads, cfg.head_dim, cfg.ffn, cfg.vocab, cfg.rank,
-                  BF16 if cfg.wdtype == "bf16" else F32, BF16 if cfg.kvdtype == "bf16" else F32,
+                  BF16 if cfg.wdtype == "bf16" else F32, KV_DTYPES[cfg.kvdtype],
                   cfg.rms_eps, cfg.rope_theta, cfg.n_experts, cfg.top_k, cfg.expert_ffn, slots,
                   getattr(cfg, "fast_heads", 0), getattr(cfg, "fast_topk", 0), int(getattr(cfg, "fast_mlp_adapter", 0)),
                   getattr(cfg, "head_rank", 0))
@@ -230,7 +232,9 @@ def cache_replay(n_layers: int, n_experts: int, top_k: int, slots: int, slow: np
 class PagedKV:
     """Paged slow-stream KV cache in device memory (caller-owned, per the ABI):
     pages ``[n_layers][num_blocks][H][block_size][hd]``, one block table
-    ``[n_seqs][max_blocks_per_seq]`` shared by all layers."""
+    ``[n_seqs][max_blocks_per_seq]`` shared by all layers.  ``kvdtype`` "fp8":
+    e4m3 codes with scales ``[n_layers][num_blocks][H]``; ``pages8`` gives a layer
+    to the operators of ``kv8``."""
 
     def __init__(self, cfg, n_seqs: int, max_ctx: int, *, block_size: int = 16, block_table=None,
                  num_blocks: Optional[int] = None, device="cuda"):
@@ -244,10 +248,14 @@ class PagedKV:
         block_table = np.asarray(block_table, np.int32)
         assert block_table.shape == (n_seqs, self.max_blocks_per_seq)
         self.num_blocks = int(num_blocks if num_blocks is not None else block_table.max() + 1)
-        dt = torch.bfloat16 if cfg.kvdtype == "bf16" else torch.float32
+        dt = {"f32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.float8_e4m3fn}[cfg.kvdtype]
         shape = (cfg.n_layers, self.num_blocks, cfg.n_heads, block_size, cfg.head_dim)
         self.k = torch.zeros(shape, dtype=dt, device=device)
         self.v = torch.zeros(shape, dtype=dt, device=device)
+        self.k_scales = self.v_scales = None
+        if cfg.kvdtype == "fp8":
+            self.k_scales = torch.ones(shape[:3], device=device)
+            self.v_scales = torch.ones(shape[:3], device=device)
         self.block_table_np = block_table
         self.block_table = torch.tensor(block_table, device=device)
         self.seq_lens = torch.zeros(n_seqs, dtype=torch.int32, device=device)
@@ -255,15 +263,32 @@ class PagedKV:
     def desc(self, seq: int = 0) -> KV:
         """Descriptor whose first sequence is block-table row `seq`."""
         return KV(self.k.data_ptr(), self.v.data_ptr(), self.block_table[seq:].data_ptr(),
-                  self.seq_lens[seq:].data_ptr(), self.num_blocks, self.block_size, self.max_blocks_per_seq)
+                  self.seq_lens[seq:].data_ptr(), self.num_blocks, self.block_size, self.max_blocks_per_seq,
+                  _ptr(self.k_scales), _ptr(self.v_scales))
+
+    def pages8(self, layer: int):
+        """A layer of an 8-bit cache (``kv8.KV8Pages``)."""
+        from .kv8 import KV8Pages
+        return KV8Pages(self.k[layer], self.v[layer], self.k_scales[layer], self.v_scales[layer], self.block_table)
 
     def _index(self, seq: int, positions: np.ndarray):
         blk = self.block_table_np[seq][positions // self.block_size]
         return blk, positions % self.block_size
 
     def load(self, seq: int, layer: int, K: np.ndarray, V: np.ndarray, start: int = 0) -> None:
-        """Store ``K/V [T][H][hd]`` at positions start.. of a sequence."""
+        """Store ``K/V [T][H][hd]`` at positions start.. of a sequence (an 8-bit
+        cache: quantised as ``kv8_append`` does, which does it)."""
         import torch
+        if self.k_scales is not None:
+            from .kv8 import kv8_append
+            n = len(self.block_table_np)
+            rows = torch.zeros(n + 1, dtype=torch.int32)
+            rows[seq + 1:] = K.shape[0]
+            pos = torch.zeros(n, dtype=torch.int32)
+            pos[seq] = start
+            k, v = (torch.tensor(np.ascontiguousarray(x, np.float32)).to(self.k.device) for x in (K, V))
+            kv8_append(self.pages8(layer), k, v, rows.to(self.k.device), pos.to(self.k.device))
+            return
         blk, slot = self._index(seq, np.arange(start, start + K.shape[0]))
         bi = torch.tensor(blk, device=self.k.device, dtype=torch.long)
         si = torch.tensor(slot, device=self.k.device, dtype=torch.long)
@@ -276,7 +301,14 @@ class PagedKV:
         blk, slot = self._index(seq, np.arange(start, end))
         bi = torch.tensor(blk, device=self.k.device, dtype=torch.long)
         si = torch.tensor(slot, device=self.k.device, dtype=torch.long)
-        return (self.k[layer, bi, :, si, :].double().cpu().numpy(), self.v[layer, bi, :, si, :].double().cpu().numpy())
+        out = []
+        for x, s in ((self.k, self.k_scales), (self.v, self.v_scales)):
+            if s is None:
+                y = x[layer, bi, :, si, :].double()
+            else:
+                y = x[layer].view(torch.uint8)[bi, :, si, :].view(x.dtype).double() * s[layer, bi].double()[..., None]
+            out.append(y.cpu().numpy())
+        return tuple(out)
 
 
 class Model:

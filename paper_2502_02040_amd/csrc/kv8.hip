@@ -6,6 +6,7 @@
 #include <cmath>
 
 #include "kv8_append.h"
+#include "kv8_cut.h"
 #include "kv8_few.h"
 #include "kv8_many.h"
 #include "m2r2_kv8.h"
@@ -81,44 +82,9 @@ void append_launch(const Kv8AppArgs& A, hipStream_t st) {
   else k8_append<BF, HD, 4, 4><<<(unsigned)units, kKv8AppThreads, 0, st>>>(A);
 }
 
-// How a call of attention is cut up.
-struct Cut {
-  bool many;       // k8_many
-  int cols;        // of a tile
-  int target;      // workgroups, about
-  int max_splits;  // of a tile
-  int pcols;       // columns of a partial result
-  long long entries;
-  size_t bytes;    // of the workspace
-};
-
-// Sixteen columns a sequence on average and k8_few: more would read the cache
-// once for every sixteen.
-constexpr int kFewMost = 16;
-
-Cut cut(const m2r2_kv8* kv, int n_seqs, int n_rows, int n_heads, int dtype) {
-  Cut c;
-  const int group = n_heads / kv->n_kv_heads, H = kv->n_kv_heads;
-  const long long cols = (long long)n_rows * group;
-  c.many = cols > (long long)kFewMost * std::max(1, n_seqs);
-  c.cols = c.many ? kManyCols : kFewCols;
-  // what a compute unit holds: two workgroups, three of k8_few's bfloat16 form
-  c.target = (c.many || dtype == M2R2_F32 ? 2 : 3) * kKv8Units;
-  // joins cost a little per split: 32, or what gives every compute unit one
-  c.max_splits = (int)std::max(32LL, std::min<long long>(kKv8MaxSplits, kKv8Units / std::max(1LL, (long long)n_seqs * H)));
-  c.pcols = c.many ? kManyCols : (int)std::min<long long>(kFewCols, std::max<long long>(1, cols));
-  const long long tiles = std::min<long long>(n_seqs, n_rows) + cols / c.cols;   // at most: ceil(a) <= a + 1 where a > 0
-  const long long cap = (long long)kv->max_blocks_per_seq * kv->block_size;
-  const long long most = tiles * std::min<long long>(c.max_splits, (cap + kKv8MinTokens - 1) / kKv8MinTokens);
-  c.entries = std::min(most, kv8_share(c.target, H) + tiles);
-  const long long slots = std::min(most, 2LL * kv8_share(c.target, H));
-  c.bytes = sizeof(uint32_t) * kKv8Counters + sizeof(float) * slots * H * kv8_part_floats(c.pcols, kv->head_dim);
-  return c;
-}
-
 template <int BF, int HD>
 void few_launch(const Kv8AttnArgs& A, hipStream_t st) {
-  k8_few<BF, HD><<<(unsigned)(A.entries * A.kv.H), kFewThreads, 0, st>>>(A);
+  k8_few<BF, HD><<<(unsigned)(A.entries * A.kv.H), kFewThreads, 0, st>>>(A, Kv8Out<BF, HD>{});
 }
 
 constexpr int kMaxDevices = 64;
@@ -201,7 +167,7 @@ M2R2_API m2r2_status m2r2_kv8_workspace_size(const m2r2_kv8* kv, int32_t n_seqs,
     return set_error(M2R2_E_SHAPE, "n_seqs %d, n_rows %d", n_seqs, n_rows);
   if (!bytes_out) return set_error(M2R2_E_INVALID, "bytes_out is NULL");
   if ((long long)n_rows * n_heads >= 1LL << 31) return set_error(M2R2_E_SHAPE, "n_rows * n_heads reaches 2^31");
-  const Cut c = cut(kv, n_seqs, n_rows, n_heads, M2R2_BF16);   // (the larger)
+  const Kv8Cut c = kv8_cut(pages(kv), kv->head_dim, n_seqs, n_rows, n_heads, 1);   // (the larger)
   if (c.entries * kv->n_kv_heads >= 1LL << 31) return set_error(M2R2_E_SHAPE, "too many rows and heads for one call");
   *bytes_out = c.bytes;
   return M2R2_OK;
@@ -240,12 +206,8 @@ M2R2_API m2r2_status m2r2_kv8_attention(const m2r2_kv8* kv, const m2r2_kv8_query
   A.scale = a->scale > 0.f ? a->scale : 1.f / sqrtf((float)kv->head_dim);
   A.err = a->err_d;
   A.group = a->n_heads / kv->n_kv_heads;
-  const Cut c = cut(kv, a->n_seqs, a->n_rows, a->n_heads, a->dtype);
-  A.cnt = (uint32_t*)workspace;
-  A.part = (float*)((char*)workspace + sizeof(uint32_t) * kKv8Counters);
-  A.pcols = c.pcols; A.target = c.target; A.max_splits = c.max_splits; A.entries = (int)c.entries;
-  const uint32_t d = kv->block_size / kKv8Slab;
-  A.bs_magic = ((1u << 31) + d - 1) / d;
+  const Kv8Cut c = kv8_cut(A.kv, kv->head_dim, a->n_seqs, a->n_rows, a->n_heads, a->dtype == M2R2_BF16);
+  kv8_cut_args(A, c, workspace);
   if (c.many) {
     hipError_t e = hipSuccess;
     M2R2_KV8_DISPATCH(many_launch, a->dtype == M2R2_BF16, kv->head_dim, A, stream, &e);

@@ -75,6 +75,32 @@ __device__ __forceinline__ float kv8_scaled(float y, float inv) {
   return kv8_finite(y) ? fminf(fmaxf(y, -kTop), kTop) * inv : __uint_as_float(0x7fc00000u);
 }
 
+// Eight codes at `p` whose scale grew, times f (a power of two).
+__device__ __forceinline__ void kv8_regrow(uint8_t* p, float f) {
+  const uint2 c = *(const uint2*)p;
+  uint2 o;
+  const auto c0 = __builtin_amdgcn_cvt_pk_f32_fp8(c.x, false), c1 = __builtin_amdgcn_cvt_pk_f32_fp8(c.x, true);
+  const auto c2 = __builtin_amdgcn_cvt_pk_f32_fp8(c.y, false), c3 = __builtin_amdgcn_cvt_pk_f32_fp8(c.y, true);
+  o.x = kv8_pack4(c0[0] * f, c0[1] * f, c1[0] * f, c1[1] * f);
+  o.y = kv8_pack4(c2[0] * f, c2[1] * f, c3[0] * f, c3[1] * f);
+  *(uint2*)p = o;
+}
+// Eight values of each half, as codes.
+__device__ __forceinline__ void kv8_store16(uint8_t* p, int half, const float (&y)[16], float inv) {
+  float z[16];
+#pragma unroll
+  for (int x = 0; x < 16; ++x) z[x] = kv8_scaled(y[x], inv);
+  *(uint2*)p = make_uint2(kv8_pack4(z[0], z[1], z[2], z[3]), kv8_pack4(z[4], z[5], z[6], z[7]));
+  *(uint2*)(p + half) = make_uint2(kv8_pack4(z[8], z[9], z[10], z[11]), kv8_pack4(z[12], z[13], z[14], z[15]));
+}
+// Maximum of their magnitudes, not counting NaN and infinities.
+__device__ __forceinline__ float kv8_most16(const float (&y)[16]) {
+  float m = 0.f;
+#pragma unroll
+  for (int x = 0; x < 16; ++x) m = fmaxf(m, kv8_finite(y[x]) ? fabsf(y[x]) : 0.f);
+  return m;
+}
+
 // WPU: waves per unit; NIT: slabs of 16 tokens per wave, at most.
 template <int BF, int HD, int WPU, int NIT>
 __global__ __launch_bounds__(kKv8AppThreads) void k8_append(Kv8AppArgs A) {
@@ -206,8 +232,8 @@ __global__ __launch_bounds__(kKv8AppThreads) void k8_append(Kv8AppArgs A) {
           }
           y[i][t][x] = a;
           y[i][t][8 + x] = b;
-          most = fmaxf(most, fmaxf(kv8_finite(a) ? fabsf(a) : 0.f, kv8_finite(b) ? fabsf(b) : 0.f));
         }
+        most = fmaxf(most, kv8_most16(y[i][t]));
       }
     most = wave_max(most);
     if constexpr (WPU > 1) {
@@ -227,17 +253,8 @@ __global__ __launch_bounds__(kKv8AppThreads) void k8_append(Kv8AppArgs A) {
         for (int t = 0; t < NS; ++t) {
           const int slot = slot_of(i, t), d = dim_of(t);
           if (slot >= first) continue;
-#pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            uint2* p = (uint2*)(base + slot * HD + z * HALF + d);
-            const uint2 c = *p;
-            uint2 o;
-            const auto c0 = __builtin_amdgcn_cvt_pk_f32_fp8(c.x, false), c1 = __builtin_amdgcn_cvt_pk_f32_fp8(c.x, true);
-            const auto c2 = __builtin_amdgcn_cvt_pk_f32_fp8(c.y, false), c3 = __builtin_amdgcn_cvt_pk_f32_fp8(c.y, true);
-            o.x = kv8_pack4(c0[0] * f, c0[1] * f, c1[0] * f, c1[1] * f);
-            o.y = kv8_pack4(c2[0] * f, c2[1] * f, c3[0] * f, c3[1] * f);
-            *p = o;
-          }
+          kv8_regrow(base + slot * HD + d, f);
+          kv8_regrow(base + slot * HD + HALF + d, f);
         }
     }
 #pragma unroll
@@ -246,12 +263,7 @@ __global__ __launch_bounds__(kKv8AppThreads) void k8_append(Kv8AppArgs A) {
       for (int t = 0; t < NS; ++t) {
         const int slot = slot_of(i, t), d = dim_of(t);
         if (slot < first || slot >= last) continue;
-        float z[16];
-#pragma unroll
-        for (int x = 0; x < 16; ++x) z[x] = kv8_scaled(y[i][t][x], inv);
-        *(uint2*)(base + slot * HD + d) = make_uint2(kv8_pack4(z[0], z[1], z[2], z[3]), kv8_pack4(z[4], z[5], z[6], z[7]));
-        *(uint2*)(base + slot * HD + HALF + d) =
-            make_uint2(kv8_pack4(z[8], z[9], z[10], z[11]), kv8_pack4(z[12], z[13], z[14], z[15]));
+        kv8_store16(base + slot * HD + d, HALF, y[i][t], inv);
       }
     if (lane == 0 && wv == 0 && (first == 0 || grown)) *scale = kv8_two_to(e);
   }

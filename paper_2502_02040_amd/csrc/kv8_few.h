@@ -245,19 +245,28 @@ struct Kv8Few {
 // Floats of a partial result: the columns' accumulators, then their maxima and sums.
 __host__ __device__ constexpr int kv8_part_floats(int cols, int hd) { return cols * (hd + 2); }
 
-template <int BF>
-__device__ __forceinline__ void kv8_emit2(const Kv8AttnArgs& A, int row, int head, int d, float a, float b) {
-  const int64_t to = (int64_t)row * A.out_row + (int64_t)head * A.out_head + d;
-  if constexpr (BF) *(uint32_t*)((uint16_t*)A.out + to) = kv8_pk(a, b);
-  else *(float2*)((float*)A.out + to) = make_float2(a, b);
-}
-
+// Where results go: the caller's array.
 template <int BF, int HD>
-__global__ __launch_bounds__(kFewThreads, 2) void k8_few(Kv8AttnArgs A) {
+struct Kv8Out {
+  static constexpr bool kKeep = false;   // results of a tile are wanted together, in LDS
+  struct Ahead {};                       // what finish() reads, requested early
+  __device__ __forceinline__ void request(Ahead&, const Kv8AttnArgs&, int) const {}
+  __device__ __forceinline__ void put(const Kv8AttnArgs& A, int row, int head, int d, float a, float b) const {
+    const int64_t to = (int64_t)row * A.out_row + (int64_t)head * A.out_head + d;
+    if constexpr (BF) *(uint32_t*)((uint16_t*)A.out + to) = kv8_pk(a, b);
+    else *(float2*)((float*)A.out + to) = make_float2(a, b);
+  }
+  __device__ __forceinline__ void finish(const Ahead&, const Kv8AttnArgs&, const Kv8Work&, int, int, const float (*)[HD],
+                                         float*) const {}
+};
+
+template <int BF, int HD, class Out>
+__global__ __launch_bounds__(kFewThreads, 2) void k8_few(Kv8AttnArgs A, Out out) {
   constexpr int OD = HD / 16;   // dims of a thread of the own keys
   __shared__ __attribute__((aligned(16))) float acc_s[kFewWaves][kFewCols][HD];
   __shared__ float m_s[kFewWaves][kFewCols], l_s[kFewWaves][kFewCols];
-  __shared__ float ov_s[kFewCols][HD], oz_s[kFewCols];   // own values and scores (first split)
+  __shared__ __attribute__((aligned(16))) float ov_s[kFewCols][HD];
+  __shared__ float oz_s[kFewCols];   // own values and scores (first split)
   __shared__ float mw[kFewCols][kKv8MaxSplits], li_s[kFewCols];
   __shared__ int last_s;
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -278,6 +287,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void k8_few(Kv8AttnArgs A) {
   const int ntile = t1 > w.t0 ? (t1 - w.t0 + kFewTile - 1) / kFewTile : 0;
   const float sc = A.scale * kLog2e;
   F f;
+  typename Out::Ahead ahead;
   typename F::Tile ta, tb;
   typename F::Places pa, pb;
   typename F::Blocks bn;
@@ -310,6 +320,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void k8_few(Kv8AttnArgs A) {
     if (part == 0) oz_s[oc] = has ? z : -INFINITY;
   }
   f.init(A, w, h, c);
+  out.request(ahead, A, h);
   // Tiles that every live column sees whole; the next tile's codes are in flight
   // meanwhile, whatever kind it is.
   const int nfull = min(ntile, max(0, (least - w.t0) / kFewTile));
@@ -376,14 +387,20 @@ __global__ __launch_bounds__(kFewThreads, 2) void k8_few(Kv8AttnArgs A) {
       }
     }
     if (w.splits == 1) {
-      kv8_emit2<BF>(A, w.r0 + (c0 + i) / A.group, h * A.group + (c0 + i) % A.group, d, kv8_over(a, l), kv8_over(b, l));
+      a = kv8_over(a, l);
+      b = kv8_over(b, l);
+      out.put(A, w.r0 + (c0 + i) / A.group, h * A.group + (c0 + i) % A.group, d, a, b);
+      if (Out::kKeep) *(float2*)&ov_s[i][d] = make_float2(a, b);   // (read above, by this thread)
     } else {
       float* p = part + (int64_t)w.split * pstep;
       st_agent2(p + e, a, b);
       if (d == 0) st_agent2(p + A.pcols * HD + 2 * i, M, l);
     }
   }
-  if (w.splits == 1) return;
+  if (w.splits == 1) {
+    out.finish(ahead, A, w, h, live, ov_s, &mw[0][0]);
+    return;
+  }
   // ---- the last split to arrive joins them ---------------------------------------
   if (!arrive_last(A.cnt + w.unit * A.kv.H + h, w.splits, &last_s)) return;
   // Pairs of dims; where a column or two leave threads over, groups of threads
@@ -438,10 +455,13 @@ __global__ __launch_bounds__(kFewThreads, 2) void k8_few(Kv8AttnArgs A) {
       }
     }
     if (grp == 0 && e < pairs) {
-      kv8_emit2<BF>(A, w.r0 + (c0 + i) / A.group, h * A.group + (c0 + i) % A.group, 2 * e - i * HD,
-                    kv8_over(a, li_s[i]), kv8_over(b, li_s[i]));
+      a = kv8_over(a, li_s[i]);
+      b = kv8_over(b, li_s[i]);
+      out.put(A, w.r0 + (c0 + i) / A.group, h * A.group + (c0 + i) % A.group, 2 * e - i * HD, a, b);
+      if (Out::kKeep) *(float2*)&ov_s[i][2 * e - i * HD] = make_float2(a, b);
     }
   }
+  out.finish(ahead, A, w, h, live, ov_s, &mw[0][0]);
 }
 
 }  // namespace m2r2

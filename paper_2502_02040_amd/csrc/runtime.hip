@@ -28,6 +28,8 @@
 #include "arla.h"
 #include "persist.h"
 #include "flops.h"
+#include "kv8_cut.h"
+#include "kv8_path.h"
 #include "status.h"
 
 using namespace m2r2;
@@ -128,11 +130,13 @@ struct Layout {
   size_t moe_logits, moe_sel, moe_prob, moe_act, moe_slots, moe_tab, moe_hits;
   size_t expert_bytes, expert_stride;
   int TD, TF, TV, S_max;
+  size_t k8_q, k8_ok, k8_ov, k8_meta, k8_part, k8_cnt;   // 8-bit cache: rows, k8_few's arrays and workspace
   size_t sk_slots;                       // partial-sum slots of the stream-K GEMVs
   int lm_slots;                          // arg-max partial slots (per LM-head tile or workgroup)
 };
 
 bool is_moe(const m2r2_config& c) { return c.n_experts > 0; }
+bool is_kv8(const m2r2_config& c) { return c.kvdtype == M2R2_FP8; }
 bool is_flops(const m2r2_config& c) {
   return c.fast_heads > 0 || c.fast_topk > 0 || c.fast_mlp_adapter != 0 || c.head_rank > 0;
 }
@@ -278,6 +282,14 @@ Layout make_layout(const m2r2_config& c, int max_batch, int max_chunk, int max_c
   L.fsc = take(flops ? sizeof(float) * (size_t)fh * max_ctx : 0);
   L.fqkv = take(flops ? sizeof(float) * (size_t)fh * 3 * c.head_dim : 0);
   L.lrz = take(sizeof(float) * std::max(c.head_rank, 1));
+  // 8-bit cache: queries, own keys and values, the rows' description, partial results
+  const bool kv8 = is_kv8(c);
+  L.k8_q = take(kv8 ? sizeof(float) * kMaxRows * qdim : 0);
+  L.k8_ok = take(kv8 ? sizeof(float) * max_batch * qdim : 0);
+  L.k8_ov = take(kv8 ? sizeof(float) * max_batch * qdim : 0);
+  L.k8_meta = take(kv8 ? sizeof(int) * kKv8Meta : 0);
+  L.k8_part = take(kv8 ? sizeof(float) * 2 * kv8_share(2 * kKv8Units, c.n_heads) * c.n_heads *
+                             kv8_part_floats(kFewCols, c.head_dim) : 0);
   // activations in operand order (passes of 3 and more rows, bf16 weights)
   const bool planes = wb && !moe;
   const size_t planes0 = off;
@@ -293,6 +305,7 @@ Layout make_layout(const m2r2_config& c, int max_batch, int max_chunk, int max_c
   L.sk_cnt = take(sizeof(uint32_t) * (65 + std::max({L.TD, L.TF, L.TV, 3 * ((qdim + 15) / 16) + (3 * r + 15) / 16})));
   L.pk_bar = take(sizeof(uint32_t) * kPkRelStride * kPkGroups);
   L.pk_rel = take(sizeof(uint32_t) * kPkRelStride * kPkGroups);
+  L.k8_cnt = take(kv8 ? sizeof(uint32_t) * kKv8Counters : 0);
   L.scratch_end = off;
   // ---- context state: sticky error bits, RoPE table, expert cache
   L.err = take(sizeof(int));
@@ -316,7 +329,10 @@ Layout make_layout(const m2r2_config& c, int max_batch, int max_chunk, int max_c
 m2r2_status check_config(const m2r2_config* c, int max_batch, int max_chunk, int max_ctx) {
   if (!c) return fail(M2R2_E_INVALID, "config is NULL");
   if (c->wdtype != M2R2_F32 && c->wdtype != M2R2_BF16) return fail(M2R2_E_DTYPE, "wdtype %d", c->wdtype);
-  if (c->kvdtype != M2R2_F32 && c->kvdtype != M2R2_BF16) return fail(M2R2_E_DTYPE, "kvdtype %d", c->kvdtype);
+  if (c->kvdtype != M2R2_F32 && c->kvdtype != M2R2_BF16 && !is_kv8(*c))
+    return fail(M2R2_E_DTYPE, "kvdtype %d", c->kvdtype);
+  if (is_kv8(*c) && (is_moe(*c) || is_flops(*c)))
+    return fail(M2R2_E_UNSUPPORTED, "an 8-bit cache is for dense models in the memory-bound form");
   const int kstep = c->wdtype == M2R2_BF16 ? 32 : 16;
   if (c->n_layers < 1 || c->n_layers > 127) return fail(M2R2_E_SHAPE, "n_layers %d not in [1,127]", c->n_layers);
   if (c->d_model <= 0 || c->d_model % kstep) return fail(M2R2_E_SHAPE, "d_model %d not a multiple of %d", c->d_model, kstep);
@@ -451,6 +467,9 @@ struct m2r2_ctx {
     uint32_t *bar = nullptr, *rel = nullptr;
     const LayerPtrs* layers_d = nullptr;
   } pk;
+  Kv8Path k8{};                  // 8-bit cache: scratch of a pass
+  float* k8_part = nullptr;
+  uint32_t* k8_cnt = nullptr;
   SkPlan sk[5];
   SkWS skws{};
   int timed_class = -1;
@@ -476,13 +495,20 @@ m2r2_status check_kv(const m2r2_ctx* c, const m2r2_kv* kv) {
   if (kv->num_blocks < 1 || kv->block_size < 1 || kv->max_blocks_per_seq < 1)
     return fail(M2R2_E_SHAPE, "kv sizes");
   if (!aligned16(kv->k_pages) || !aligned16(kv->v_pages)) return fail(M2R2_E_INVALID, "kv pages not 16-byte aligned");
-  (void)c;
+  if (is_kv8(c->cfg)) {
+    if (!kv->k_scales || !kv->v_scales) return fail(M2R2_E_INVALID, "an 8-bit cache's k_scales or v_scales is NULL");
+    if (kv->block_size % kKv8Slab || kv->block_size > 256)
+      return fail(M2R2_E_SHAPE, "block_size %d not a multiple of 16 in [16,256]", kv->block_size);
+    if ((long long)kv->num_blocks * c->D.H * kv->block_size >= 1LL << 31 ||
+        (long long)kv->max_blocks_per_seq * kv->block_size >= 1LL << 30)
+      return fail(M2R2_E_SHAPE, "the pool holds 2^31 rows of a layer, or a sequence 2^30 positions");
+  }
   return M2R2_OK;
 }
 
 KVPtrs kv_ptrs(const m2r2_kv* kv) {
   return KVPtrs{kv->k_pages, kv->v_pages, kv->block_table_d, kv->seq_lens_d, kv->num_blocks, kv->block_size,
-                kv->max_blocks_per_seq};
+                kv->max_blocks_per_seq, kv->k_scales, kv->v_scales};
 }
 
 constexpr int kMaxTimed = 1024;
@@ -710,6 +736,30 @@ void mf_launch(const m2r2_ctx* c, const LayerPtrs& L, const RowMap& rm, const St
   else km_attn<WB, HD, 16><<<grid, kMfThreads, lds, st>>>(c->D, L, rm, c->ws, io, kv, l, S);
 }
 
+// The 8-bit cache: the rows formed and appended, then attention over them.
+template <int WB, int HD>
+void kv8_launch(const m2r2_ctx* c, const LayerPtrs& L, const RowMap& rm, const StepIO& io, const KVPtrs& kv, int l,
+                hipStream_t st) {
+  const Dims& D = c->D;
+  k8_rows<WB, HD><<<dim3(D.H, rm.nseq), 256, 0, st>>>(D, L, rm, c->ws, io, kv, l, c->k8);
+  const size_t pages = (size_t)l * kv.num_blocks * D.H;   // of the layers before
+  Kv8AttnArgs A{};
+  A.kv = Kv8Pages{(uint8_t*)kv.k + pages * kv.bs * HD, (uint8_t*)kv.v + pages * kv.bs * HD, kv.ks + pages, kv.vs + pages,
+                  kv.bt, kv.num_blocks, kv.bs, kv.mbps, D.H};
+  A.n_seqs = rm.nseq; A.n_rows = rm.M; A.n_heads = D.H; A.group = 1;
+  A.row_start = c->k8.row_start; A.lens = c->k8.lens; A.visible = c->k8.visible; A.own = c->k8.own;
+  A.q = c->k8.q; A.q_row = D.qdim; A.q_head = HD;
+  A.own_k = c->k8.ok; A.own_v = c->k8.ov; A.n_own = rm.nseq;
+  A.ok_row = A.ov_row = D.qdim; A.ok_head = A.ov_head = HD;
+  A.scale = 1.f / sqrtf((float)HD);
+  A.err = c->ws.err;
+  const Kv8Cut cut = kv8_cut(A.kv, HD, rm.nseq, rm.M, D.H, false);   // (at most 16 rows a sequence: few columns)
+  kv8_cut_args(A, cut, nullptr);
+  A.cnt = c->k8_cnt;
+  A.part = c->k8_part;
+  k8_few<0, HD><<<(unsigned)(A.entries * D.H), kFewThreads, 0, st>>>(A, Kv8PathOut<WB, HD>{D, rm, c->ws, L.A[3]});
+}
+
 // Attention of a pass with one or two rows: on the matrix cores where that
 // applies (SM splits), else the short-chain kernel up to its 64 splits, else
 // the general one (a bfloat16 cache whose capacity has more: pages of 2^31
@@ -747,7 +797,9 @@ m2r2_status run_layers_rw(m2r2_ctx* c, const RowMap& rm, const StepIO& io, const
   for (int l = 0; l < n_layers_run; ++l) {
     const LayerPtrs& L = c->layers[l];
     TIMED(0, (kr_qkv_launch<WB>(nd, G, lds, st, D, L, rm, c->ws, io, l)));
-    if (S2 > 0)
+    if (is_kv8(c->cfg))
+      TIMED(1, (kv8_launch<WB, HD>(c, L, rm, io, kv, l, st)));
+    else if (S2 > 0)
       TIMED(1, (ks_attn<WB, KB, HD, 2><<<dim3(S2, D.H, rm.nseq), kSkAttnThreads, sk_attn_lds_bytes(HD, D.r, WB),
                                           st>>>(D, L, rm, c->ws, io, kv, l, S2)));
     else
@@ -771,8 +823,10 @@ m2r2_status run_layers_sk(m2r2_ctx* c, const RowMap& rm, const StepIO& io, const
   int rows_per_seq = 1;
   for (int s = 0; s < rm.nseq; ++s) rows_per_seq = std::max(rows_per_seq, (int)rm.cnt[s]);
   const int S = choose_splits(rm.nseq, rows_per_seq, D.H, c->max_ctx);
-  if (S > c->lay.S_max) return fail(M2R2_E_SHAPE, "attention splits exceed the workspace");
-  if (S + 1 > 64) return fail(M2R2_E_SHAPE, "context too long for the attention merge (max_ctx %d)", c->max_ctx);
+  const bool kv8 = is_kv8(c->cfg);
+  if (!kv8 && S > c->lay.S_max) return fail(M2R2_E_SHAPE, "attention splits exceed the workspace");
+  if (!kv8 && S + 1 > 64)
+    return fail(M2R2_E_SHAPE, "context too long for the attention merge (max_ctx %d)", c->max_ctx);
   const size_t smem = attn_smem_bytes();
   const int G = c->sk_grid;
   const size_t ld = sk_lds(D.d), lq = sk_lds(D.qdim), lf = sk_lds(D.F);
@@ -781,7 +835,9 @@ m2r2_status run_layers_sk(m2r2_ctx* c, const RowMap& rm, const StepIO& io, const
   for (int l = 0; l < n_layers_run; ++l) {
     const LayerPtrs& L = c->layers[l];
     TIMED(0, (ks_qkv<WB><<<G, kSkThreads, ld, st>>>(D, L, rm, c->ws, io, c->sk[0], sk, l)));
-    if (c->sk_attn_S)
+    if (kv8)
+      TIMED(1, (kv8_launch<WB, HD>(c, L, rm, io, kv, l, st)));
+    else if (c->sk_attn_S)
       TIMED(1, (ks_attn<WB, KB, HD><<<dim3(c->sk_attn_S, D.H, rm.nseq), kSkAttnThreads,
                                        sk_attn_lds_bytes(HD, D.r, WB), st>>>(D, L, rm, c->ws, io, kv, l, c->sk_attn_S)));
     else
@@ -869,7 +925,8 @@ m2r2_status run_layers_t(m2r2_ctx* c, const RowMap& rm, const StepIO& io, const 
   // attention: on the matrix cores where that applies (SM below); else one or
   // two rows per sequence (batched decoding) take the short-chain kernel with
   // fixed splits, longer chunks the general one
-  const bool short_attn = c->sk_attn_S > 0 && rows_per_seq <= 2;
+  const bool kv8 = is_kv8(c->cfg);   // (an 8-bit cache has its own)
+  const bool short_attn = kv8 || (c->sk_attn_S > 0 && rows_per_seq <= 2);
   // many splits in flight (batched long contexts): two 128-token chunks per
   // split, the second chunk's loads overlapping the first chunk's work
   const int NCA = c->attn_chunks != 0 ? c->attn_chunks
@@ -890,7 +947,9 @@ m2r2_status run_layers_t(m2r2_ctx* c, const RowMap& rm, const StepIO& io, const 
     const LayerPtrs& L = c->layers[l];
     if constexpr (TP) TIMED(0, (tp_qkv<MT>(c, L, rm, io, l, st)));
     else TIMED(0, (k_qkv<WB, MT><<<G.qkv, kGemvThreads, G.l_d, st>>>(D, L, rm, c->ws, io, l)));
-    if (SM > 0)
+    if (kv8)
+      TIMED(1, (kv8_launch<WB, HD>(c, L, rm, io, kv, l, st)));
+    else if (SM > 0)
       TIMED(1, (mf_launch<WB, HD>(c, L, rm, io, kv, l, SM, rows_per_seq, st)));
     else if (short_attn && S2 > 0 && NCA == 4)
       TIMED(1, (ks_attn<WB, KB, HD, 4><<<dim3(S2, D.H, rm.nseq), kSkAttnThreads, sk_attn_lds_bytes(HD, D.r, WB),
@@ -1142,7 +1201,7 @@ hipError_t sk_setup(m2r2_ctx* c) {
     const int Ks[3] = {D.d, D.qdim, D.F};
     // (a capacity of more splits than the short-chain attention has: the matrix-core one)
     const bool ok_m = D.kvbf16 && !is_flops(cf) && (c->max_ctx + kMfMaxTokens - 1) / kMfMaxTokens <= std::min(63, c->lay.S_max);
-    bool ok_r = (c->sk_attn_S > 0 || ok_m) && (D.r * wsz) % 16 == 0 && D.r * wsz <= kRwMaxBRowBytes &&
+    bool ok_r = (c->sk_attn_S > 0 || ok_m || is_kv8(cf)) && (D.r * wsz) % 16 == 0 && D.r * wsz <= kRwMaxBRowBytes &&
                 !getenv_zero("M2R2_ROWWAVE");
     for (int i = 0; i < (moe ? 2 : 3); ++i) {
       c->rw_nch[i] = Ks[i] / epp;
@@ -1188,6 +1247,7 @@ hipError_t pk_attr(size_t lds, int* per_cu) {
 // within 64, every head at least one attention split, one workgroup per
 // compute unit resident.
 hipError_t pk_setup(m2r2_ctx* c) {
+  if (is_kv8(c->cfg)) return hipSuccess;   // (an 8-bit cache is appended to in a launch of its own)
   c->pk.kind = -1;
   const Dims& D = c->D;
   // M2R2_ONE_LAUNCH=0 keeps one sequence on the multi-kernel path
@@ -1820,6 +1880,13 @@ M2R2_API m2r2_status m2r2_create(const m2r2_config* cfg, const m2r2_weights* w, 
   ws.rope = (const float2*)(b + lay.rope);
   ws.rope_len = max_ctx;
   ws.fsc = (float*)(b + lay.fsc); ws.fqkv = (float*)(b + lay.fqkv); ws.lrz = (float*)(b + lay.lrz);
+  if (is_kv8(*cfg)) {
+    int* m = (int*)(b + lay.k8_meta);
+    c->k8 = Kv8Path{(float*)(b + lay.k8_q), (float*)(b + lay.k8_ok), (float*)(b + lay.k8_ov), m, m + kMaxSeq + 1,
+                    m + 2 * kMaxSeq + 1, m + 2 * kMaxSeq + 1 + kMaxRows};
+    c->k8_part = (float*)(b + lay.k8_part);
+    c->k8_cnt = (uint32_t*)(b + lay.k8_cnt);
+  }
   c->skws.part = (float*)(b + lay.sk_part);
   c->skws.hier = (uint32_t*)(b + lay.sk_cnt);
   c->skws.cnt = c->skws.hier + 65;
@@ -2062,7 +2129,11 @@ struct ScratchRebase {
   WS ws;
   SkWS sk;
   decltype(m2r2_ctx::pk) pk;
-  ScratchRebase(m2r2_ctx* ctx, char* dst) : c(ctx), ws(ctx->ws), sk(ctx->skws), pk(ctx->pk) {
+  Kv8Path k8;
+  float* k8_part;
+  uint32_t* k8_cnt;
+  ScratchRebase(m2r2_ctx* ctx, char* dst)
+      : c(ctx), ws(ctx->ws), sk(ctx->skws), pk(ctx->pk), k8(ctx->k8), k8_part(ctx->k8_part), k8_cnt(ctx->k8_cnt) {
     const char* lo = c->ws_base + c->lay.scratch_begin;
     const char* hi = c->ws_base + c->lay.scratch_end;
     auto rb = [&](auto* p) {
@@ -2077,6 +2148,10 @@ struct ScratchRebase {
     w.arla_kv = rb(w.arla_kv); w.arla_q = rb(w.arla_q); w.arla_sig = rb(w.arla_sig); w.arla_cnt = rb(w.arla_cnt);
     w.XB = rb(w.XB); w.OB = rb(w.OB); w.AB = rb(w.AB);
     w.fsc = rb(w.fsc); w.fqkv = rb(w.fqkv); w.lrz = rb(w.lrz);
+    Kv8Path& k = c->k8;
+    k.q = rb(k.q); k.ok = rb(k.ok); k.ov = rb(k.ov); k.row_start = rb(k.row_start); k.lens = rb(k.lens);
+    k.visible = rb(k.visible); k.own = rb(k.own);
+    c->k8_part = rb(c->k8_part); c->k8_cnt = rb(c->k8_cnt);
     c->skws.part = rb(c->skws.part); c->skws.hier = rb(c->skws.hier); c->skws.cnt = rb(c->skws.cnt);
     c->pk.sd = rb(c->pk.sd); c->pk.so = rb(c->pk.so); c->pk.sgu = rb(c->pk.sgu); c->pk.bar = rb(c->pk.bar); c->pk.rel = rb(c->pk.rel);
   }
@@ -2084,6 +2159,9 @@ struct ScratchRebase {
     c->ws = ws;
     c->skws = sk;
     c->pk = pk;
+    c->k8 = k8;
+    c->k8_part = k8_part;
+    c->k8_cnt = k8_cnt;
   }
 };
 

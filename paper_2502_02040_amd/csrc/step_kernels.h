@@ -82,6 +82,7 @@ struct KVPtrs {
   const int* bt;     // [nseq][mbps]
   int* seq_lens;
   int num_blocks, bs, mbps;
+  float *ks, *vs;    // scales of an 8-bit cache (kv8.h)
 };
 
 // Workspace views (all device pointers).
