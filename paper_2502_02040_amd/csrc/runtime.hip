@@ -741,7 +741,12 @@ template <int WB, int HD>
 void kv8_launch(const m2r2_ctx* c, const LayerPtrs& L, const RowMap& rm, const StepIO& io, const KVPtrs& kv, int l,
                 hipStream_t st) {
   const Dims& D = c->D;
-  k8_rows<WB, HD><<<dim3(D.H, rm.nseq), 256, 0, st>>>(D, L, rm, c->ws, io, kv, l, c->k8);
+  int rows = 1;
+  for (int s = 0; s < rm.nseq; ++s) rows = std::max(rows, (int)rm.cnt[s]);
+  if (rows <= 2)
+    k8_rows<WB, HD, 2><<<dim3(D.H, rm.nseq), 256, 0, st>>>(D, L, rm, c->ws, io, kv, l, c->k8);
+  else
+    k8_rows<WB, HD, kMaxRows><<<dim3(D.H, rm.nseq), 256, 0, st>>>(D, L, rm, c->ws, io, kv, l, c->k8);
   const size_t pages = (size_t)l * kv.num_blocks * D.H;   // of the layers before
   Kv8AttnArgs A{};
   A.kv = Kv8Pages{(uint8_t*)kv.k + pages * kv.bs * HD, (uint8_t*)kv.v + pages * kv.bs * HD, kv.ks + pages, kv.vs + pages,
