@@ -81,51 +81,73 @@ class KV8Pages:
         self.k_pages, self.v_pages, self.k_scales, self.v_scales = k_pages, v_pages, k_scales, v_scales
         self.block_table = block_table
         nb, H, bs, hd = k_pages.shape
+        self.gpu = k_pages.get_device()   # (-1: not on one)
         self.n_seqs, self.n_kv_heads, self.head_dim = block_table.shape[0], H, hd
         self._desc = _Pages(k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
                             block_table.data_ptr(), nb, bs, block_table.shape[1], H, hd)
 
 
-def _int32s(t, n: Optional[int], name: str, device) -> Optional[int]:
-    import torch
+_torch = None
+
+
+def _t():
+    """torch, imported on first use as in ``binding``."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
+# A decoding step makes these calls for every layer, and its kernels take a few
+# microseconds each: the checks below look at every tensor once.
+
+def _int32s(t, n: int, name: str, gpu: int) -> Optional[int]:
+    """Pointer to a vector of at least n int32 on the GPU (None: NULL)."""
     if t is None:
         return None
-    if t.dtype is not torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.device != device:
-        raise ValueError(f"{name}: a contiguous int32 vector on {device}")
-    if n is not None and t.shape[0] < n:
-        raise ValueError(f"{name}: {t.shape[0]} entries, {n} needed")
+    sh = t.shape
+    if len(sh) != 1 or sh[0] < n or t.dtype is not _t().int32 or t.stride()[0] != 1 or t.get_device() != gpu:
+        raise ValueError(f"{name}: a contiguous int32 vector of at least {n} entries on GPU {gpu}, "
+                         f"not {t.dtype} {tuple(sh)} on {t.device}")
     return t.data_ptr()
 
 
-def _rows(t, name: str, like, heads: int, kv: KV8Pages, n: Optional[int] = None):
-    """(pointer, row stride, head stride) of a [rows][heads][head_dim] tensor."""
-    sh, st = t.shape, t.stride()
-    if len(sh) != 3 or sh[1] != heads or sh[2] != kv.head_dim or st[2] != 1 or (n is not None and sh[0] != n):
-        raise ValueError(f"{name}: shape {tuple(sh)}, strides {tuple(st)}")
-    if t.dtype != like.dtype or t.device != kv.device:
-        raise ValueError(f"{name}: {t.dtype} on {t.device}")
-    return t.data_ptr(), st[0], st[1]
+def _rows(t, name: str, n: int, heads: int, hd: int, dtype, gpu: int):
+    """(pointer, row stride, head stride) of a [n][heads][hd] tensor."""
+    row, head, dim = t.stride() if t.dim() == 3 else (0, 0, 0)
+    if t.shape != (n, heads, hd) or dim != 1 or t.dtype is not dtype or t.get_device() != gpu:
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, strides {tuple(t.stride())} on {t.device}; "
+                         f"expected {dtype} ({n}, {heads}, {hd}) with adjacent dims on GPU {gpu}")
+    return t.data_ptr(), row, head
 
 
-def _dtype(t, name: str) -> int:
-    import torch
-    if t.dtype is torch.bfloat16:
-        return BF16
-    if t.dtype is torch.float32:
-        return F32
-    raise ValueError(f"{name}: {t.dtype} (bfloat16 or float32)")
+def _dtype(t, name: str):
+    torch = _t()
+    dt = t.dtype
+    if dt is torch.bfloat16:
+        return BF16, dt
+    if dt is torch.float32:
+        return F32, dt
+    raise ValueError(f"{name}: {dt} (bfloat16 or float32)")
 
 
-def _call(fn, where: str, device, stream, *args) -> None:
-    import torch
-    if device.type != "cuda":
-        raise ValueError(f"{where}: tensors on {device}")
-    s = (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
-    if torch.cuda.current_device() == device.index:
-        _check(fn(*args, s), where)
+def _call(fn, where: str, kv, stream, *args) -> None:
+    """fn(*args, stream) with the cache's GPU current."""
+    gpu, cuda = kv.gpu, _t().cuda
+    if gpu < 0:
+        raise ValueError(f"{where}: tensors on {kv.device}")
+    if stream is not None:
+        s = stream.cuda_stream
+    else:   # (the handle without a Stream object around it, which takes a microsecond)
+        s = _t()._C._cuda_getCurrentRawStream(gpu)
+    if cuda.current_device() == gpu:
+        st = fn(*args, s)
     else:
-        with torch.cuda.device(device):
-            _check(fn(*args, s), where)
+        with cuda.device(gpu):
+            st = fn(*args, s)
+    if st:
+        _check(st, where)
 
 
 def kv8_append(kv: KV8Pages, k, v, row_start, positions, *, rope=None, q=None, q_out=None, errors=None,
@@ -135,27 +157,28 @@ def kv8_append(kv: KV8Pages, k, v, row_start, positions, *, rope=None, q=None, q
     ``rope`` [length][head_dim/2][2] float32 (cos, sin) turns the keys (and the
     queries ``q`` [rows][heads][head_dim] into ``q_out``, which may be ``q``).
     ``errors``: an int32 tensor into which the kernels or error bits."""
-    import torch
-    n = k.shape[0]
-    pk = _rows(k, "k", k, kv.n_kv_heads, kv)
-    pv = _rows(v, "v", k, kv.n_kv_heads, kv, n)
-    heads, pq, po = 0, (None, 0, 0), (None, 0, 0)
-    if (q is None) != (q_out is None):
-        raise ValueError("q and q_out come together")
-    if q is not None:
+    n, H, hd, ns, gpu = k.shape[0], kv.n_kv_heads, kv.head_dim, kv.n_seqs, kv.gpu
+    code, dt = _dtype(k, "k")
+    kp, k_row, k_head = _rows(k, "k", n, H, hd, dt, gpu)
+    vp, v_row, v_head = _rows(v, "v", n, H, hd, dt, gpu)
+    heads, qp, q_row, q_head, op, o_row, o_head = 0, None, 0, 0, None, 0, 0
+    if q is not None and q_out is not None:
         heads = q.shape[1]
-        pq, po = _rows(q, "q", k, heads, kv, n), _rows(q_out, "q_out", k, heads, kv, n)
-    rlen = 0
+        qp, q_row, q_head = _rows(q, "q", n, heads, hd, dt, gpu)
+        op, o_row, o_head = _rows(q_out, "q_out", n, heads, hd, dt, gpu)
+    elif q is not None or q_out is not None:
+        raise ValueError("q and q_out come together")
+    rp, rlen = None, 0
     if rope is not None:
-        if (rope.dim() != 3 or rope.shape[1:] != (kv.head_dim // 2, 2) or rope.dtype is not torch.float32
-                or not rope.is_contiguous() or rope.device != kv.device):
-            raise ValueError("rope: a contiguous float32 tensor [length][head_dim/2][2]")
         rlen = rope.shape[0]
-    ns = kv.n_seqs
-    r = _Rows(ns, n, _int32s(row_start, ns + 1, "row_start", kv.device), _int32s(positions, ns, "positions", kv.device),
-              _dtype(k, "k"), pk[0], pv[0], pk[1], pk[2], pv[1], pv[2], None if rope is None else rope.data_ptr(), rlen,
-              heads, pq[0], po[0], pq[1], pq[2], po[1], po[2], _int32s(errors, 1, "errors", kv.device))
-    _call(_lib()[0], "m2r2_kv8_append", kv.device, stream, kv._desc, r)
+        if (rope.shape != (rlen, hd // 2, 2) or rope.dtype is not _t().float32 or not rope.is_contiguous()
+                or rope.get_device() != gpu):
+            raise ValueError("rope: a contiguous float32 tensor [length][head_dim/2][2] on the cache's GPU")
+        rp = rope.data_ptr()
+    r = _Rows(ns, n, _int32s(row_start, ns + 1, "row_start", gpu), _int32s(positions, ns, "positions", gpu), code, kp, vp,
+              k_row, k_head, v_row, v_head, rp, rlen, heads, qp, op, q_row, q_head, o_row, o_head,
+              _int32s(errors, 1, "errors", gpu))
+    _call(_lib()[0], "m2r2_kv8_append", kv, stream, kv._desc, r)
 
 
 def kv8_workspace(kv: KV8Pages, q):
@@ -174,20 +197,19 @@ def kv8_attention(kv: KV8Pages, q, row_start, lens, out, workspace, *, visible=N
     min(visible[r], lens[s]) of them (None: causal, the sequence's last row sees
     all) and, where own[r] >= 0, the key and value own_k/own_v[own[r]] beside
     them.  A row that sees nothing is zero."""
-    n, heads = q.shape[0], q.shape[1]
-    pq, po = _rows(q, "q", q, heads, kv), _rows(out, "out", q, heads, kv, n)
-    pk = pv = (None, 0, 0)
-    n_own = 0
+    n, heads, H, hd, ns, gpu = q.shape[0], q.shape[1], kv.n_kv_heads, kv.head_dim, kv.n_seqs, kv.gpu
+    code, dt = _dtype(q, "q")
+    qp, q_row, q_head = _rows(q, "q", n, heads, hd, dt, gpu)
+    op, o_row, o_head = _rows(out, "out", n, heads, hd, dt, gpu)
+    n_own, kp, k_row, k_head, vp, v_row, v_head = 0, None, 0, 0, None, 0, 0
     if own is not None:
         n_own = own_k.shape[0]
-        pk = _rows(own_k, "own_k", q, kv.n_kv_heads, kv)
-        pv = _rows(own_v, "own_v", q, kv.n_kv_heads, kv, n_own)
-    ns, dev = kv.n_seqs, kv.device
-    if workspace.device != dev or not workspace.is_contiguous():
-        raise ValueError(f"workspace: a contiguous tensor on {dev}")
-    a = _Query(ns, n, _int32s(row_start, ns + 1, "row_start", dev), _int32s(lens, ns, "lens", dev),
-               _int32s(visible, n, "visible", dev), _dtype(q, "q"), heads, pq[0], pq[1], pq[2],
-               _int32s(own, n, "own", dev), pk[0], pv[0], n_own, pk[1], pk[2], pv[1], pv[2],
-               0.0 if scale is None else scale, po[0], po[1], po[2], _int32s(errors, 1, "errors", dev))
-    _call(_lib()[2], "m2r2_kv8_attention", dev, stream, kv._desc, a, workspace.data_ptr(),
-          workspace.numel() * workspace.element_size())
+        kp, k_row, k_head = _rows(own_k, "own_k", n_own, H, hd, dt, gpu)
+        vp, v_row, v_head = _rows(own_v, "own_v", n_own, H, hd, dt, gpu)
+    if workspace.get_device() != gpu or not workspace.is_contiguous():
+        raise ValueError(f"workspace: a contiguous tensor on GPU {gpu}")
+    a = _Query(ns, n, _int32s(row_start, ns + 1, "row_start", gpu), _int32s(lens, ns, "lens", gpu),
+               _int32s(visible, n, "visible", gpu), code, heads, qp, q_row, q_head, _int32s(own, n, "own", gpu), kp, vp,
+               n_own, k_row, k_head, v_row, v_head, 0.0 if scale is None else scale, op, o_row, o_head,
+               _int32s(errors, 1, "errors", gpu))
+    _call(_lib()[2], "m2r2_kv8_attention", kv, stream, kv._desc, a, workspace.data_ptr(), workspace.nbytes)
