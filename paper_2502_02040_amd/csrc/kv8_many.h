@@ -17,6 +17,8 @@
 // a second part would cost half of all products again.  Those of float32 rows
 // are kept to 24 bits.
 #pragma once
+#include <type_traits>
+
 #include "kv8_few.h"
 
 namespace m2r2 {
@@ -42,8 +44,19 @@ __device__ __forceinline__ f32x16_t kv8_mma32(u32x4_t a, u32x4_t b, f32x16_t c) 
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c,
                                                  0, 0, 0);
 }
-__device__ __forceinline__ float kv8_swap32(float v) {   // the other half's value
-  return __shfl_xor(v, 32);
+// Maximum and sum of lanes l and l ^ 32.
+__device__ __forceinline__ float kv8_max32(float v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float kv8_sum32(float v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+// v plus both bfloat16 of w.
+__device__ __forceinline__ float kv8_add2(uint32_t w, float v) {
+  const bf16x2_t one = __builtin_bit_cast(bf16x2_t, 0x3f803f80u);
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w), one, v, false);
 }
 
 template <int BF, int HD>
@@ -68,8 +81,7 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
   const int row = w.r0 + cc / A.group, head = h * A.group + cc % A.group;
   const int sees = kv8_sees(A, w, c);
   // of the wave's columns, and of the workgroup's (a tile's 128 columns: every thread looks at all)
-  int most = sees, least = live ? sees : 1 << 30;
-  int most_all = 0, least_all = 1 << 30;
+  int most = sees, most_all = 0, least_all = 1 << 30;
 #pragma unroll
   for (int x = 0; x < kManyCols / 64; ++x) {
     const int o = c0 + 64 * x + lane, v = kv8_sees(A, w, o);
@@ -79,12 +91,10 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     most = max(most, __shfl_xor(most, d));
-    least = min(least, __shfl_xor(least, d));
     most_all = max(most_all, __shfl_xor(most_all, d));
     least_all = min(least_all, __shfl_xor(least_all, d));
   }
   most = __builtin_amdgcn_readfirstlane(most);
-  least = __builtin_amdgcn_readfirstlane(least);
   most_all = __builtin_amdgcn_readfirstlane(most_all);
   least_all = __builtin_amdgcn_readfirstlane(least_all);
   const int t1 = min(w.t1, most_all);
@@ -102,38 +112,34 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
   };
   // block ids of a tile, requested a tile before its codes
   struct Ids {
-    int k, v;
-  };
-  auto slot = [&](int tp, int& in) {   // logical block of a position (the last one where the table ends)
-    const uint32_t lb = (uint32_t)(((uint64_t)((uint32_t)tp >> 4) * A.bs_magic) >> 31);
-    in = tp - (int)lb * A.kv.bs;
-    return min((int)lb, A.kv.mbps - 1);
+    int k, v, kin, vin;   // block, position in it
   };
   const int* bt = A.kv.bt + (int64_t)w.s * A.kv.mbps;
   auto ask = [&](int tt) {
     const int t = w.t0 + tt * kManyTile;
-    int in;
-    return Ids{bt[slot(t + kt, in)], bt[slot(t + vt, in)]};
-  };
-  auto fetch = [&](int tt, const Ids& id, Raw& r) {
-    const int t = w.t0 + tt * kManyTile;
-    auto place = [&](int blk, int tp, int& rw, bool& ok) {
-      int in;
-      slot(tp, in);
-      ok = (uint32_t)blk < (uint32_t)A.kv.nb;
-      if (!ok && tp < t1 && tt < ntile) kv8_error(A.err, KV8_ERR_BLOCK);
-      const int page = (ok ? blk : 0) * A.kv.H + h;
-      rw = page * A.kv.bs + in;
-      return page;
+    Ids id;
+    auto slot = [&](int tp, int& in) {   // logical block (the last one where the table ends)
+      const uint32_t lb = (uint32_t)(((uint64_t)((uint32_t)tp >> 4) * A.bs_magic) >> 31);
+      in = tp - (int)lb * A.kv.bs;
+      return min((int)lb, A.kv.mbps - 1);
     };
-    int rk, rv;
-    const int pk = place(id.k, t + kt, rk, r.kok), pv = place(id.v, t + vt, rv, r.vok);
-    r.ks = A.kv.ks[pk];
-    r.vs = A.kv.vs[pv];
-    const uint8_t* kp = A.kv.k + (int64_t)rk * HD + kd;
+    id.k = bt[slot(t + kt, id.kin)];
+    id.v = bt[slot(t + vt, id.vin)];
+    return id;
+  };
+  const uint32_t page = A.kv.H * A.kv.bs * HD;   // bytes of a block
+  const uint8_t* kb = A.kv.k + (int64_t)h * A.kv.bs * HD + kd;
+  const uint8_t* vb = A.kv.v + (int64_t)h * A.kv.bs * HD + min(vd, HD - 8);
+  auto fetch = [&](const Ids& id, Raw& r) {
+    r.kok = (uint32_t)id.k < (uint32_t)A.kv.nb;
+    r.vok = (uint32_t)id.v < (uint32_t)A.kv.nb;
+    const uint32_t bk = r.kok ? id.k : 0, bv = r.vok ? id.v : 0;
+    r.ks = A.kv.ks[bk * A.kv.H + h];
+    r.vs = A.kv.vs[bv * A.kv.H + h];
+    const uint8_t* kp = kb + (uint64_t)bk * page + id.kin * HD;
 #pragma unroll
     for (int x = 0; x < NK; ++x) r.k[x] = kv8_ld<u32x2_t>(kp + 8 * x);
-    const uint8_t* vp = A.kv.v + (int64_t)rv * HD + min(vd, HD - 8);
+    const uint8_t* vp = vb + (uint64_t)bv * page + id.vin * HD;
 #pragma unroll
     for (int x = 0; x < 4; ++x) r.v[x] = kv8_ld<u32x2_t>(vp + x * HD);
   };
@@ -143,7 +149,10 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
       S.gap[(tt + 2) & 3] = 0;
       S.odd[(tt + 2) & 3] = 0;
     }
-    if (!r.kok) atomicOr(&S.gap[tt & 3], 1ull << kt);
+    if (!r.kok) {
+      atomicOr(&S.gap[tt & 3], 1ull << kt);
+      if (t + kt < t1) kv8_error(A.err, KV8_ERR_BLOCK);
+    }
 #pragma unroll
     for (int x = 0; x < NK; ++x) {
       const u32x4_t o = {kv8_up<false>(r.k[x][0], r.ks), kv8_up<true>(r.k[x][0], r.ks), kv8_up<false>(r.k[x][1], r.ks),
@@ -208,91 +217,110 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
   }
   __syncthreads();
   Raw ra;
-  Ids id{0, 0};
+  Ids id{};
   if (ntile > 0) {
     const Ids i0 = ask(0), i1 = ask(1);
-    fetch(0, i0, ra);
+    fetch(i0, ra);
     stage(0, ra, 0);
-    fetch(1, i1, ra);   // (beyond the last tile: some position's block, staged nowhere)
+    fetch(i1, ra);   // (beyond the last tile: some position's block, staged nowhere)
     id = ask(2);
   }
   __syncthreads();
   // row m of a product is this position of its 32
   const int krow = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
-  for (int tt = 0; tt < ntile; ++tt) {
+  // FULL: every live column of the workgroup sees all of the tile, and it is all there
+  auto compute = [&](int tt, auto full) {
+    constexpr bool FULL = decltype(full)::value;
     const int buf = tt & 1, t0 = w.t0 + tt * kManyTile;
-    if (t0 < most) {
-      const unsigned long long gap = S.gap[tt & 3] >> (8 * hi);
-      const bool full = t0 + kManyTile <= least && !__any(gap != 0);
-      f32x16_t sa[2];
+    f32x16_t sa[2];
+#pragma unroll
+    for (int s = 0; s < NQ; ++s) {
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
+        const u32x4_t k = *(const u32x4_t*)&S.k[buf][(32 * x + krow) * KP + 16 * s + 8 * hi];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sa[x][r] = 0.f;
+        for (int p = QN - 1; p >= 0; --p)
+          sa[x] = s == 0 && p == QN - 1 ? kv8_mma32(k, q[s][p], f32x16_t{}) : kv8_mma32(k, q[s][p], sa[x]);
       }
+    }
+    // keys are read ahead of the products, or every product waits for the LDS
+    if constexpr (BF) {
+      constexpr int AHEAD = 6;
+      __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
 #pragma unroll
-      for (int s = 0; s < NQ; ++s) {
+      for (int i = 0; i < 2 * NQ - AHEAD; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x8, AHEAD, 0);
+    }
+    // lane (column n, hi): scores of positions 32 x + 16 (r / 8) + 8 hi + r % 8
+    const int lim = min(sees, t1) - t0;
+    float mx = -INFINITY;
+    if constexpr (!FULL) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (32 * x + 16 * (r >> 3) + (r & 7) >= lim - 8 * hi) sa[x][r] = -INFINITY;
+      if (const unsigned long long gap = S.gap[tt & 3]) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          const u32x4_t k = *(const u32x4_t*)&S.k[buf][(32 * x + krow) * KP + 16 * s + 8 * hi];
+          const uint32_t half = (uint32_t)(gap >> (32 * x)) >> (8 * hi);
 #pragma unroll
-          for (int p = QN - 1; p >= 0; --p) sa[x] = kv8_mma32(k, q[s][p], sa[x]);
+          for (int r = 0; r < 16; ++r)
+            if ((half >> (16 * (r >> 3) + (r & 7))) & 1) sa[x][r] = -INFINITY;
         }
       }
-      // lane (column n, hi): scores of positions 32 x + 16 (r / 8) + 8 hi + r % 8
-      float mx = -INFINITY;
-      if (full) {
+    }
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+    for (int x = 0; x < 2; ++x)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sa[x][r]);
-      } else {
-        const int lim = min(sees, t1) - t0 - 8 * hi;
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int at = 32 * x + 16 * (r >> 3) + (r & 7);
-            if (at >= lim || ((gap >> at) & 1)) sa[x][r] = -INFINITY;
-            mx = fmaxf(mx, sa[x][r]);
-          }
-      }
-      mx = fmaxf(mx, kv8_swap32(mx)) * sc;
-      const float mn = fmaxf(m_run, mx);
-      const float mb = mn == -INFINITY ? 0.f : mn;
-      const float al = __builtin_amdgcn_exp2f(m_run - mb);
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sa[x][r]);
+    mx = kv8_max32(mx) * sc;
+    // The maximum moves only when a score is more than 2^8 times above it:
+    // weights of up to 2^8 are as exact as those of up to 1, and the
+    // accumulators are seldom scaled.
+    if (__any(mx > m_run + 8.f)) {
+      const float mn = mx > m_run + 8.f ? mx : m_run;   // (m_run -infinity: nothing seen yet)
+      const float al = mn == m_run ? 1.f : __builtin_amdgcn_exp2f(m_run - mn);
       m_run = mn;
-      float ls = 0.f;
-      u32x4_t pb[4][PN];
+      l_run *= al;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        float p[8];
+      for (int d = 0; d < NO; ++d)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sa[u >> 1][8 * (u & 1) + i], sc, -mb));
-          ls += p[i];
-        }
-        kv8_parts<PN>(p, pb[u]);
+        for (int r = 0; r < 16; ++r) acc[d][r] *= al;
+    }
+    const float mb = !FULL && m_run == -INFINITY ? 0.f : m_run;
+    u32x4_t pb[4][PN];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      float p[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sa[u >> 1][8 * (u & 1) + i], sc, -mb));
+      kv8_parts<PN>(p, pb[u]);
+      // the sum is that of the weights as they are used
+      if constexpr (PN == 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) l_run = kv8_add2(pb[u][0][i], l_run);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) l_run += p[i];
       }
-      l_run = l_run * al + ls;
-      if (__any(al != 1.f)) {
+    }
 #pragma unroll
-        for (int d = 0; d < NO; ++d)
+    for (int u = 0; u < 4; ++u)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) acc[d][r] *= al;
+      for (int d = 0; d < NO; ++d) {
+        const u32x4_t v = *(const u32x4_t*)&S.v[buf][(32 * d + n) * VP + 16 * u + 8 * hi];
+#pragma unroll
+        for (int p = PN - 1; p >= 0; --p) acc[d] = kv8_mma32(v, pb[u][p], acc[d]);
       }
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int d = 0; d < NO; ++d) {
-          const u32x4_t v = *(const u32x4_t*)&S.v[buf][(32 * d + n) * VP + 16 * u + 8 * hi];
-#pragma unroll
-          for (int p = PN - 1; p >= 0; --p) acc[d] = kv8_mma32(v, pb[u][p], acc[d]);
-        }
+    if constexpr (!FULL) {
       // NaN values, which the products took as zero, for the columns that see them
       for (unsigned long long odd = S.odd[tt & 3]; odd; odd &= odd - 1) {
         const int p = __ffsll(odd) - 1;
-        if (t0 + p < min(sees, t1)) {
+        if (p < lim) {
 #pragma unroll
           for (int d = 0; d < NO; ++d)
 #pragma unroll
@@ -305,13 +333,24 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
         }
       }
     }
+  };
+  auto advance = [&](int tt) {   // tile tt + 1 into the other buffer, whose readers passed the last barrier
     if (tt + 1 < ntile) {
-      // (the other buffer's readers passed the last barrier)
-      stage(tt + 1, ra, buf ^ 1);
-      if (tt + 2 < ntile) fetch(tt + 2, id, ra);
+      stage(tt + 1, ra, (tt + 1) & 1);
+      fetch(id, ra);   // (as above)
       id = ask(tt + 3);
       __syncthreads();
     }
+  };
+  int tt = 0;
+  const int nfull = min(ntile, max(0, (least_all - w.t0) / kManyTile));
+  for (; tt < nfull && !S.gap[tt & 3]; ++tt) {
+    compute(tt, std::true_type{});
+    advance(tt);
+  }
+  for (; tt < ntile; ++tt) {
+    if (w.t0 + tt * kManyTile < most) compute(tt, std::false_type{});
+    advance(tt);
   }
   // ---- results -----------------------------------------------------------------------
   // the own key, once
@@ -327,7 +366,7 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
       z += kv8_elem<BF>(A.q, (int64_t)row * A.q_row + (int64_t)head * A.q_head + dd) *
            kv8_elem<BF>(A.own_k, (int64_t)oo * A.ok_row + (int64_t)h * A.ok_head + dd);
     }
-    z = (z + kv8_swap32(z)) * sc;
+    z = kv8_sum32(z) * sc;
     if (!has) z = -INFINITY;
     const float mn = fmaxf(m_run, z), mb = mn == -INFINITY ? 0.f : mn;
     const float al = __builtin_amdgcn_exp2f(m_run - mb), p = has ? __builtin_amdgcn_exp2f(z - mb) : 0.f;
@@ -342,7 +381,7 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
         if (has) acc[d][r] += p * kv8_elem<BF>(A.own_v, (int64_t)oo * A.ov_row + (int64_t)h * A.ov_head + dim);
       }
   }
-  const float l_all = l_run + kv8_swap32(l_run);
+  const float l_all = kv8_sum32(l_run);
   auto put = [&](int d, int r, float a, float b, float e, float f) {   // four dims of the lane's column
     const int64_t to = (int64_t)row * A.out_row + (int64_t)head * A.out_head + 32 * d + 8 * (r >> 2) + 4 * hi;
     if constexpr (BF) *(u32x2_t*)((uint16_t*)A.out + to) = u32x2_t{kv8_pk(a, b), kv8_pk(e, f)};
