@@ -30,15 +30,20 @@ constexpr int kManyThreads = 256;
 template <int HD>
 struct Kv8ManyLds {
   static constexpr int KP = HD + 8;           // padded rows (elements): 16 lanes' 16 bytes hit all banks
-  static constexpr int VP = kManyTile + 8;
   uint16_t k[2][kManyTile * KP];              // [position][dim]
-  uint16_t v[2][HD * VP];                     // [dim][position]
+  uint16_t v[2][HD * kManyTile];              // [dim][position], kv8_at_v
   // of a tile (four in turn): positions outside the pool; positions with NaN
   // values, of a tile that not all columns see whole, and which dims' they are
   unsigned long long gap[4], odd[4];
+  int gaps;                                   // any of the first
   uint8_t nan[2][kManyTile][HD / 8];
   int last;
 };
+
+// Place of positions 8 c .. 8 c + 7 of dim d: the eight 16-byte pieces of a
+// row are permuted by its number, so that neither eight rows at one piece (the
+// products' reads) nor sixteen rows eight apart (the transposed writes) meet in a bank.
+__device__ __forceinline__ int kv8_at_v(int d, int c) { return d * kManyTile + 8 * (c ^ (d & 7) ^ (d >> 3 & 7)); }
 
 __device__ __forceinline__ f32x16_t kv8_mma32(u32x4_t a, u32x4_t b, f32x16_t c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c,
@@ -65,9 +70,8 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
   constexpr int NO = HD / 32;                // tiles of 32 output dims
   constexpr int QN = BF ? 1 : 3, PN = BF ? 1 : 3;
   using L = Kv8ManyLds<HD>;
-  constexpr int KP = L::KP, VP = L::VP;
-  constexpr int NK = HD / 32;                // 8-byte pieces of keys per thread: positions 4 threads each
-  constexpr int ND = HD / 8;                 // groups of 8 dims: values are staged by 16 ND threads
+  constexpr int KP = L::KP;
+  constexpr int NK = HD / 32;                // 8-byte pieces of keys per thread
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
   L& S = *(L*)lds_raw;
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -102,70 +106,62 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
   const float sc = A.scale * kLog2e;
 
   // ---- staging ------------------------------------------------------------------
-  // keys: thread (position tid / 4, part tid % 4) takes HD / 4 bytes; values:
-  // thread (positions 4 (tid % 16) .., dims 8 (tid / 16) ..) takes 4 x 8 bytes
-  const int kt = tid >> 2, kd = (tid & 3) * (HD / 4), vt = (tid & 15) * 4, vd = (tid >> 4) * 8;
+  // A wave stages 16 positions, which lie in one block: where they are is the
+  // same for all lanes.  Keys: lane (position lane / 4, part lane % 4) takes
+  // HD / 4 bytes; values: lane (positions 4 (lane % 4) .., dims 8 (lane / 4) ..) takes 4 x 8 bytes.
+  const int kt = 16 * wv + (lane >> 2), kd = (lane & 3) * (HD / 4);
+  const int vt = 16 * wv + 4 * (lane & 3), vd = 8 * (lane >> 2);
+  const int vdd = min(vd, HD - 8);
+  const uint32_t koff = (lane >> 2) * HD + kd, voff = 4 * (lane & 3) * HD + vdd;
   struct Raw {
     u32x2_t k[NK], v[4];
     float ks, vs;
-    bool kok, vok;   // the place exists
-  };
-  // block ids of a tile, requested a tile before its codes
-  struct Ids {
-    int k, v, kin, vin;   // block, position in it
+    bool ok;   // the place exists
   };
   const int* bt = A.kv.bt + (int64_t)w.s * A.kv.mbps;
-  auto ask = [&](int tt) {
-    const int t = w.t0 + tt * kManyTile;
-    Ids id;
-    auto slot = [&](int tp, int& in) {   // logical block (the last one where the table ends)
-      const uint32_t lb = (uint32_t)(((uint64_t)((uint32_t)tp >> 4) * A.bs_magic) >> 31);
-      in = tp - (int)lb * A.kv.bs;
-      return min((int)lb, A.kv.mbps - 1);
-    };
-    id.k = bt[slot(t + kt, id.kin)];
-    id.v = bt[slot(t + vt, id.vin)];
-    return id;
+  // Vector loads all the same: they return in order, and the LDS's counter is the scalar loads' too.
+  auto slot = [&](int tt, int& in) {   // logical block of the wave's positions (the last one where the table ends)
+    const int tp = w.t0 + tt * kManyTile + 16 * wv;
+    const uint32_t lb = (uint32_t)(((uint64_t)((uint32_t)tp >> 4) * A.bs_magic) >> 31);
+    in = tp - (int)lb * A.kv.bs;
+    return min((int)lb, A.kv.mbps - 1);
   };
-  const uint32_t page = A.kv.H * A.kv.bs * HD;   // bytes of a block
-  const uint8_t* kb = A.kv.k + (int64_t)h * A.kv.bs * HD + kd;
-  const uint8_t* vb = A.kv.v + (int64_t)h * A.kv.bs * HD + min(vd, HD - 8);
-  auto fetch = [&](const Ids& id, Raw& r) {
-    r.kok = (uint32_t)id.k < (uint32_t)A.kv.nb;
-    r.vok = (uint32_t)id.v < (uint32_t)A.kv.nb;
-    const uint32_t bk = r.kok ? id.k : 0, bv = r.vok ? id.v : 0;
-    r.ks = A.kv.ks[bk * A.kv.H + h];
-    r.vs = A.kv.vs[bv * A.kv.H + h];
-    const uint8_t* kp = kb + (uint64_t)bk * page + id.kin * HD;
-#pragma unroll
-    for (int x = 0; x < NK; ++x) r.k[x] = kv8_ld<u32x2_t>(kp + 8 * x);
-    const uint8_t* vp = vb + (uint64_t)bv * page + id.vin * HD;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) r.v[x] = kv8_ld<u32x2_t>(vp + x * HD);
+  int zero = 0;   // (an offset that the compiler takes for a vector)
+  asm("" : "+v"(zero));
+  auto ask = [&](int tt) {   // block id, requested a tile before the codes
+    int in;
+    return kv8_ld<int>(bt + slot(tt, in) + zero);
   };
-  auto stage = [&](int tt, Raw& r, int buf) {
-    const int t = w.t0 + tt * kManyTile;
-    if (tid == 0) {   // marks that were last read two tiles ago
-      S.gap[(tt + 2) & 3] = 0;
-      S.odd[(tt + 2) & 3] = 0;
-    }
-    if (!r.kok) {
-      atomicOr(&S.gap[tt & 3], 1ull << kt);
-      if (t + kt < t1) kv8_error(A.err, KV8_ERR_BLOCK);
-    }
+  auto fetch = [&](int tt, int id, Raw& r) {
+    int in;
+    slot(tt, in);
+    const int blk = __builtin_amdgcn_readfirstlane(id);
+    r.ok = (uint32_t)blk < (uint32_t)A.kv.nb;
+    const int page = (r.ok ? blk : 0) * A.kv.H + h;
+    r.ks = kv8_ld<float>(A.kv.ks + page + zero);
+    r.vs = kv8_ld<float>(A.kv.vs + page + zero);
+    const int64_t at = ((int64_t)page * A.kv.bs + in) * HD;
+    const uint8_t *kp = A.kv.k + at, *vp = A.kv.v + at;
 #pragma unroll
-    for (int x = 0; x < NK; ++x) {
-      const u32x4_t o = {kv8_up<false>(r.k[x][0], r.ks), kv8_up<true>(r.k[x][0], r.ks), kv8_up<false>(r.k[x][1], r.ks),
-                         kv8_up<true>(r.k[x][1], r.ks)};
-      *(u32x4_t*)&S.k[buf][kt * KP + kd + 8 * x] = o;
-    }
-    if (vd < HD) {
-      if (t + kManyTile > least_all || !r.vok) {
-        // what no column sees is zero in the products, and so is NaN, which must
-        // not reach the columns that do not see it
+    for (int x = 0; x < NK; ++x) r.k[x] = kv8_ld<u32x2_t>(kp + koff + 8 * x);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) r.v[x] = kv8_ld<u32x2_t>(vp + voff + x * HD);
+  };
+  bool gaps = false;   // some position of the split is outside the pool
+  auto clean = [&](int tt, Raw& r, int buf) {   // a tile that not every column sees whole
+    const int t = w.t0 + tt * kManyTile;
+    {
+      // What no column sees is zero in the products, and so is NaN, which must
+      // not reach the columns that do not see it.
+      if (tid == 0) {   // marks that were last read two tiles ago
+        S.gap[(tt + 2) & 3] = 0;
+        S.odd[(tt + 2) & 3] = 0;
+      }
+      if (!r.ok && lane == 0) atomicOr(&S.gap[tt & 3], 0xffffull << (16 * wv));
+      {
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          const bool there = t + vt + x < t1 && r.vok;
+          const bool there = t + vt + x < t1 && r.ok;
           uint32_t bits = 0;
 #pragma unroll
           for (int z = 0; z < 2; ++z) {
@@ -173,26 +169,38 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
             r.v[x][z] = there ? r.v[x][z] & ~nan : 0u;
             bits |= ((nan & 1) | (nan >> 7 & 2) | (nan >> 14 & 4) | (nan >> 21 & 8)) << (4 * z);
           }
-          S.nan[buf][vt + x][vd / 8] = bits;
+          S.nan[buf][vt + x][vdd / 8] = bits;
           if (bits) atomicOr(&S.odd[tt & 3], 1ull << (vt + x));
         }
       }
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        uint32_t o[4][2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t a = __builtin_amdgcn_perm(r.v[2 * i + 1][x], r.v[2 * i][x], 0x05010400u);
-          const uint32_t b = __builtin_amdgcn_perm(r.v[2 * i + 1][x], r.v[2 * i][x], 0x07030602u);
-          o[0][i] = kv8_up<false>(a, r.vs);
-          o[1][i] = kv8_up<true>(a, r.vs);
-          o[2][i] = kv8_up<false>(b, r.vs);
-          o[3][i] = kv8_up<true>(b, r.vs);
-        }
-#pragma unroll
-        for (int d = 0; d < 4; ++d) *(u32x2_t*)&S.v[buf][(vd + 4 * x + d) * VP + vt] = u32x2_t{o[d][0], o[d][1]};
-      }
     }
+  };
+  // Piece j of a tile into LDS: 8-byte pieces of the keys, then two dims at a time of the values.
+  constexpr int NPIECE = NK + 4;
+  auto piece = [&](int j, const Raw& r, int buf) {
+    if (j < NK) {
+      const u32x4_t o = {kv8_up<false>(r.k[j][0], r.ks), kv8_up<true>(r.k[j][0], r.ks), kv8_up<false>(r.k[j][1], r.ks),
+                         kv8_up<true>(r.k[j][1], r.ks)};
+      *(u32x4_t*)&S.k[buf][kt * KP + kd + 8 * j] = o;
+      return;
+    }
+    const int x = (j - NK) >> 1, z = (j - NK) & 1;
+    u32x2_t o[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t w2 = __builtin_amdgcn_perm(r.v[2 * i + 1][x], r.v[2 * i][x], z ? 0x07030602u : 0x05010400u);
+      o[0][i] = kv8_up<false>(w2, r.vs);
+      o[1][i] = kv8_up<true>(w2, r.vs);
+    }
+    // (lanes without dims write the last ones' values once more)
+#pragma unroll
+    for (int d = 0; d < 2; ++d)
+      *(u32x2_t*)&S.v[buf][kv8_at_v(vdd + 4 * x + 2 * z + d, vt >> 3) + (vt & 4)] = o[d];
+  };
+  auto stage = [&](int tt, Raw& r) {
+    if (w.t0 + (tt + 1) * kManyTile > least_all || gaps) clean(tt, r, tt & 1);
+#pragma unroll
+    for (int j = 0; j < NPIECE; ++j) piece(j, r, tt & 1);
   };
 
   // ---- queries ----------------------------------------------------------------------
@@ -214,45 +222,62 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
   if (tid < 4) {
     S.gap[tid] = 0;
     S.odd[tid] = 0;
+    S.gaps = 0;
   }
   __syncthreads();
+  for (int lb = w.t0 / A.kv.bs + tid; (int64_t)lb * A.kv.bs < t1; lb += kManyThreads)
+    if ((uint32_t)bt[lb] >= (uint32_t)A.kv.nb) {
+      S.gaps = 1;
+      kv8_error(A.err, KV8_ERR_BLOCK);
+    }
+  __syncthreads();
+  gaps = __builtin_amdgcn_readfirstlane(S.gaps) != 0;
   Raw ra;
-  Ids id{};
+  int id = 0;
   if (ntile > 0) {
-    const Ids i0 = ask(0), i1 = ask(1);
-    fetch(i0, ra);
-    stage(0, ra, 0);
-    fetch(i1, ra);   // (beyond the last tile: some position's block, staged nowhere)
+    const int i0 = ask(0), i1 = ask(1);
+    fetch(0, i0, ra);
+    stage(0, ra);
+    fetch(1, i1, ra);   // (beyond the last tile: some position's block, staged nowhere)
     id = ask(2);
   }
   __syncthreads();
   // row m of a product is this position of its 32
   const int krow = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
+  // kv8_at_v(32 d + n, 2 u + hi) is vo[u] for even d, vo[u ^ 2] for odd, plus whole rows
+  int vo[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) vo[u] = kv8_at_v(n, 2 * u + hi);
   // FULL: every live column of the workgroup sees all of the tile, and it is all there
-  auto compute = [&](int tt, auto full) {
-    constexpr bool FULL = decltype(full)::value;
+  // (so is the next one where STAGE: it is staged beside the score products,
+  // which leave the vector unit idle, and the one after requested)
+  auto compute = [&](int tt, auto full, auto beside) {
+    constexpr bool FULL = decltype(full)::value, STAGE = decltype(beside)::value;
     const int buf = tt & 1, t0 = w.t0 + tt * kManyTile;
+    // The order of this loop is meant: keys are read ahead of the products, or
+    // every product waits for the LDS, and a piece of the next tile is staged
+    // beside every other product.
+    constexpr int NM = 2 * NQ, AHEAD = NM < 6 ? NM : 6;
+    u32x4_t kf[NM];
+    auto keys = [&](int i) { return *(const u32x4_t*)&S.k[buf][(32 * (i & 1) + krow) * KP + 16 * (i >> 1) + 8 * hi]; };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) kf[i] = keys(i);
     f32x16_t sa[2];
 #pragma unroll
-    for (int s = 0; s < NQ; ++s) {
+    for (int i = 0; i < NM; ++i) {
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const u32x4_t k = *(const u32x4_t*)&S.k[buf][(32 * x + krow) * KP + 16 * s + 8 * hi];
+      for (int p = QN - 1; p >= 0; --p)
+        sa[i & 1] = i < 2 && p == QN - 1 ? kv8_mma32(kf[i], q[0][p], f32x16_t{}) : kv8_mma32(kf[i], q[i >> 1][p], sa[i & 1]);
+      if (i + AHEAD < NM) kf[i + AHEAD] = keys(i + AHEAD);
+      if constexpr (STAGE) {
 #pragma unroll
-        for (int p = QN - 1; p >= 0; --p)
-          sa[x] = s == 0 && p == QN - 1 ? kv8_mma32(k, q[s][p], f32x16_t{}) : kv8_mma32(k, q[s][p], sa[x]);
+        for (int j = i * NPIECE / NM; j < (i + 1) * NPIECE / NM; ++j) piece(j, ra, buf ^ 1);
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    // keys are read ahead of the products, or every product waits for the LDS
-    if constexpr (BF) {
-      constexpr int AHEAD = 6;
-      __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
-#pragma unroll
-      for (int i = 0; i < 2 * NQ - AHEAD; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      }
-      __builtin_amdgcn_sched_group_barrier(0x8, AHEAD, 0);
+    if constexpr (STAGE) {
+      fetch(tt + 2, id, ra);   // (beyond the last tile: some position's block, staged nowhere)
+      id = ask(tt + 3);
     }
     // lane (column n, hi): scores of positions 32 x + 16 (r / 8) + 8 hi + r % 8
     const int lim = min(sees, t1) - t0;
@@ -292,30 +317,44 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
         for (int r = 0; r < 16; ++r) acc[d][r] *= al;
     }
     const float mb = !FULL && m_run == -INFINITY ? 0.f : m_run;
-    u32x4_t pb[4][PN];
+    // Weights of 16 positions at a time, each of the products beside a pair of
+    // the next ones' weights.
+    u32x4_t pb[2][PN], vf[2][NO];
+    float ls[4] = {0.f, 0.f, 0.f, 0.f};
+    auto pair = [&](int u, int i) {   // positions 16 u + 8 hi + 2 i, + 1
+      float a = __builtin_amdgcn_exp2f(__builtin_fmaf(sa[u >> 1][8 * (u & 1) + 2 * i], sc, -mb));
+      float b = __builtin_amdgcn_exp2f(__builtin_fmaf(sa[u >> 1][8 * (u & 1) + 2 * i + 1], sc, -mb));
+      if constexpr (PN > 1) ls[i] += a + b;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      float p[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sa[u >> 1][8 * (u & 1) + i], sc, -mb));
-      kv8_parts<PN>(p, pb[u]);
-      // the sum is that of the weights as they are used
-      if constexpr (PN == 1) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) l_run = kv8_add2(pb[u][0][i], l_run);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) l_run += p[i];
+      for (int p = 0; p < PN; ++p) {
+        const uint32_t w2 = kv8_pk(a, b);
+        pb[u & 1][p][i] = w2;
+        if constexpr (PN > 1) {
+          a -= bf16lo(w2);
+          b -= bf16hi(w2);
+        }
       }
-    }
+      // (the sum is that of the weights as they are used)
+      if constexpr (PN == 1) ls[i] = kv8_add2(pb[u & 1][0][i], ls[i]);
+    };
+    auto values = [&](int u, int d) { return *(const u32x4_t*)&S.v[buf][vo[u ^ 2 * (d & 1)] + 32 * d * kManyTile]; };
+#pragma unroll
+    for (int d = 0; d < NO; ++d) vf[0][d] = values(0, d);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) pair(0, i);
 #pragma unroll
     for (int u = 0; u < 4; ++u)
 #pragma unroll
-      for (int d = 0; d < NO; ++d) {
-        const u32x4_t v = *(const u32x4_t*)&S.v[buf][(32 * d + n) * VP + 16 * u + 8 * hi];
+      for (int d = 0; d < 4; ++d) {
+        if (d < NO) {
 #pragma unroll
-        for (int p = PN - 1; p >= 0; --p) acc[d] = kv8_mma32(v, pb[u][p], acc[d]);
+          for (int p = PN - 1; p >= 0; --p) acc[d] = kv8_mma32(vf[u & 1][d], pb[u & 1][p], acc[d]);
+          if (u < 3) vf[(u + 1) & 1][d] = values(u + 1, d);
+        }
+        if (u < 3) pair(u + 1, d);
+        __builtin_amdgcn_sched_barrier(0);
       }
+    l_run += (ls[0] + ls[1]) + (ls[2] + ls[3]);
     if constexpr (!FULL) {
       // NaN values, which the products took as zero, for the columns that see them
       for (unsigned long long odd = S.odd[tt & 3]; odd; odd &= odd - 1) {
@@ -334,23 +373,20 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
       }
     }
   };
-  auto advance = [&](int tt) {   // tile tt + 1 into the other buffer, whose readers passed the last barrier
+  int tt = 0;
+  const int nfull = gaps ? 0 : min(ntile, max(0, (least_all - w.t0) / kManyTile));
+  for (; tt + 1 < nfull; ++tt) {
+    compute(tt, std::true_type{}, std::true_type{});
+    __syncthreads();   // the other buffer is staged; its readers passed the last barrier
+  }
+  for (; tt < ntile; ++tt) {
+    if (w.t0 + tt * kManyTile < most) compute(tt, std::false_type{}, std::false_type{});
     if (tt + 1 < ntile) {
-      stage(tt + 1, ra, (tt + 1) & 1);
-      fetch(id, ra);   // (as above)
+      stage(tt + 1, ra);
+      fetch(tt + 2, id, ra);
       id = ask(tt + 3);
       __syncthreads();
     }
-  };
-  int tt = 0;
-  const int nfull = min(ntile, max(0, (least_all - w.t0) / kManyTile));
-  for (; tt < nfull && !S.gap[tt & 3]; ++tt) {
-    compute(tt, std::true_type{});
-    advance(tt);
-  }
-  for (; tt < ntile; ++tt) {
-    if (w.t0 + tt * kManyTile < most) compute(tt, std::false_type{});
-    advance(tt);
   }
   // ---- results -----------------------------------------------------------------------
   // the own key, once
