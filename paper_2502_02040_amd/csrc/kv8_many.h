@@ -27,6 +27,9 @@ constexpr int kManyCols = 128;
 constexpr int kManyTile = 64;
 constexpr int kManyThreads = 256;
 
+// (the accumulators are in registers only where everything that takes them is inlined)
+#define KV8_INLINE __attribute__((always_inline))
+
 template <int HD>
 struct Kv8ManyLds {
   static constexpr int KP = HD + 8;           // padded rows (elements): 16 lanes' 16 bytes hit all banks
@@ -80,31 +83,10 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
   Kv8Work w;
   if (!kv8_pick<kManyCols>(A, entry, blockIdx.x == 0 && wv == 0, w)) return;
   const int c0 = w.tile * kManyCols, c = c0 + 32 * wv + n;
+  const bool any = c0 + 32 * wv < w.cols;   // (a wave without columns only stages)
   const bool live = c < w.cols;
   const int cc = min(c, w.cols - 1);
   const int row = w.r0 + cc / A.group, head = h * A.group + cc % A.group;
-  const int sees = kv8_sees(A, w, c);
-  // of the wave's columns, and of the workgroup's (a tile's 128 columns: every thread looks at all)
-  int most = sees, most_all = 0, least_all = 1 << 30;
-#pragma unroll
-  for (int x = 0; x < kManyCols / 64; ++x) {
-    const int o = c0 + 64 * x + lane, v = kv8_sees(A, w, o);
-    most_all = max(most_all, v);
-    least_all = min(least_all, o < w.cols ? v : 1 << 30);
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    most = max(most, __shfl_xor(most, d));
-    most_all = max(most_all, __shfl_xor(most_all, d));
-    least_all = min(least_all, __shfl_xor(least_all, d));
-  }
-  most = __builtin_amdgcn_readfirstlane(most);
-  most_all = __builtin_amdgcn_readfirstlane(most_all);
-  least_all = __builtin_amdgcn_readfirstlane(least_all);
-  const int t1 = min(w.t1, most_all);
-  const int ntile = t1 > w.t0 ? (t1 - w.t0 + kManyTile - 1) / kManyTile : 0;
-  const float sc = A.scale * kLog2e;
-
   // ---- staging ------------------------------------------------------------------
   // A wave stages 16 positions, which lie in one block: where they are is the
   // same for all lanes.  Keys: lane (position lane / 4, part lane % 4) takes
@@ -120,7 +102,7 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
   };
   const int* bt = A.kv.bt + (int64_t)w.s * A.kv.mbps;
   // Vector loads all the same: they return in order, and the LDS's counter is the scalar loads' too.
-  auto slot = [&](int tt, int& in) {   // logical block of the wave's positions (the last one where the table ends)
+  auto slot = [&](int tt, int& in) KV8_INLINE {   // logical block of the wave's positions (the last one where the table ends)
     const int tp = w.t0 + tt * kManyTile + 16 * wv;
     const uint32_t lb = (uint32_t)(((uint64_t)((uint32_t)tp >> 4) * A.bs_magic) >> 31);
     in = tp - (int)lb * A.kv.bs;
@@ -128,11 +110,33 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
   };
   int zero = 0;   // (an offset that the compiler takes for a vector)
   asm("" : "+v"(zero));
-  auto ask = [&](int tt) {   // block id, requested a tile before the codes
+  auto ask = [&](int tt) KV8_INLINE {   // block id, requested a tile before the codes
     int in;
     return kv8_ld<int>(bt + slot(tt, in) + zero);
   };
-  auto fetch = [&](int tt, int id, Raw& r) {
+  const int i0 = ask(0), i1 = ask(1);   // (needed or not)
+  const int sees = kv8_sees(A, w, c);
+  // of the wave's columns, and of the workgroup's: every thread looks at all
+  int most = sees, most_all = 0, least_all = 1 << 30;
+#pragma unroll
+  for (int x = 0; x < kManyCols / 64; ++x) {
+    const int o = c0 + 64 * x + lane, v = kv8_sees(A, w, o);
+    most_all = max(most_all, v);
+    least_all = min(least_all, o < w.cols ? v : 1 << 30);
+  }
+  auto wave_most = [](int v) {
+    v = kv8_row_max(v);
+    v = max(v, __shfl_xor(v, 16));
+    return __builtin_amdgcn_readfirstlane(max(v, __shfl_xor(v, 32)));
+  };
+  most = wave_most(most);
+  most_all = wave_most(most_all);
+  least_all = -wave_most(-least_all);
+  const int t1 = min(w.t1, most_all);
+  const int ntile = t1 > w.t0 ? (t1 - w.t0 + kManyTile - 1) / kManyTile : 0;
+  const float sc = A.scale * kLog2e;
+
+  auto fetch = [&](int tt, int id, Raw& r) KV8_INLINE {
     int in;
     slot(tt, in);
     const int blk = __builtin_amdgcn_readfirstlane(id);
@@ -147,8 +151,10 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
 #pragma unroll
     for (int x = 0; x < 4; ++x) r.v[x] = kv8_ld<u32x2_t>(vp + voff + x * HD);
   };
+  Raw ra;
+  fetch(0, i0, ra);
   bool gaps = false;   // some position of the split is outside the pool
-  auto clean = [&](int tt, Raw& r, int buf) {   // a tile that not every column sees whole
+  auto clean = [&](int tt, Raw& r, int buf) KV8_INLINE {   // a tile that not every column sees whole
     const int t = w.t0 + tt * kManyTile;
     {
       // What no column sees is zero in the products, and so is NaN, which must
@@ -177,7 +183,7 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
   };
   // Piece j of a tile into LDS: 8-byte pieces of the keys, then two dims at a time of the values.
   constexpr int NPIECE = NK + 4;
-  auto piece = [&](int j, const Raw& r, int buf) {
+  auto piece = [&](int j, const Raw& r, int buf) KV8_INLINE {
     if (j < NK) {
       const u32x4_t o = {kv8_up<false>(r.k[j][0], r.ks), kv8_up<true>(r.k[j][0], r.ks), kv8_up<false>(r.k[j][1], r.ks),
                          kv8_up<true>(r.k[j][1], r.ks)};
@@ -197,7 +203,7 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
     for (int d = 0; d < 2; ++d)
       *(u32x2_t*)&S.v[buf][kv8_at_v(vdd + 4 * x + 2 * z + d, vt >> 3) + (vt & 4)] = o[d];
   };
-  auto stage = [&](int tt, Raw& r) {
+  auto stage = [&](int tt, Raw& r) KV8_INLINE {
     if (w.t0 + (tt + 1) * kManyTile > least_all || gaps) clean(tt, r, tt & 1);
 #pragma unroll
     for (int j = 0; j < NPIECE; ++j) piece(j, r, tt & 1);
@@ -232,11 +238,8 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
     }
   __syncthreads();
   gaps = __builtin_amdgcn_readfirstlane(S.gaps) != 0;
-  Raw ra;
   int id = 0;
   if (ntile > 0) {
-    const int i0 = ask(0), i1 = ask(1);
-    fetch(0, i0, ra);
     stage(0, ra);
     fetch(1, i1, ra);   // (beyond the last tile: some position's block, staged nowhere)
     id = ask(2);
@@ -251,7 +254,7 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
   // FULL: every live column of the workgroup sees all of the tile, and it is all there
   // (so is the next one where STAGE: it is staged beside the score products,
   // which leave the vector unit idle, and the one after requested)
-  auto compute = [&](int tt, auto full, auto beside) {
+  auto compute = [&](int tt, auto full, auto beside) KV8_INLINE {
     constexpr bool FULL = decltype(full)::value, STAGE = decltype(beside)::value;
     const int buf = tt & 1, t0 = w.t0 + tt * kManyTile;
     // The order of this loop is meant: keys are read ahead of the products, or
@@ -259,7 +262,7 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
     // beside every other product.
     constexpr int NM = 2 * NQ, AHEAD = NM < 6 ? NM : 6;
     u32x4_t kf[NM];
-    auto keys = [&](int i) { return *(const u32x4_t*)&S.k[buf][(32 * (i & 1) + krow) * KP + 16 * (i >> 1) + 8 * hi]; };
+    auto keys = [&](int i) KV8_INLINE { return *(const u32x4_t*)&S.k[buf][(32 * (i & 1) + krow) * KP + 16 * (i >> 1) + 8 * hi]; };
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) kf[i] = keys(i);
     f32x16_t sa[2];
@@ -321,7 +324,7 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
     // the next ones' weights.
     u32x4_t pb[2][PN], vf[2][NO];
     float ls[4] = {0.f, 0.f, 0.f, 0.f};
-    auto pair = [&](int u, int i) {   // positions 16 u + 8 hi + 2 i, + 1
+    auto pair = [&](int u, int i) KV8_INLINE {   // positions 16 u + 8 hi + 2 i, + 1
       float a = __builtin_amdgcn_exp2f(__builtin_fmaf(sa[u >> 1][8 * (u & 1) + 2 * i], sc, -mb));
       float b = __builtin_amdgcn_exp2f(__builtin_fmaf(sa[u >> 1][8 * (u & 1) + 2 * i + 1], sc, -mb));
       if constexpr (PN > 1) ls[i] += a + b;
@@ -337,7 +340,7 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
       // (the sum is that of the weights as they are used)
       if constexpr (PN == 1) ls[i] = kv8_add2(pb[u & 1][0][i], ls[i]);
     };
-    auto values = [&](int u, int d) { return *(const u32x4_t*)&S.v[buf][vo[u ^ 2 * (d & 1)] + 32 * d * kManyTile]; };
+    auto values = [&](int u, int d) KV8_INLINE { return *(const u32x4_t*)&S.v[buf][vo[u ^ 2 * (d & 1)] + 32 * d * kManyTile]; };
 #pragma unroll
     for (int d = 0; d < NO; ++d) vf[0][d] = values(0, d);
 #pragma unroll
@@ -375,18 +378,25 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
   };
   int tt = 0;
   const int nfull = gaps ? 0 : min(ntile, max(0, (least_all - w.t0) / kManyTile));
-  for (; tt + 1 < nfull; ++tt) {
-    compute(tt, std::true_type{}, std::true_type{});
-    __syncthreads();   // the other buffer is staged; its readers passed the last barrier
-  }
-  for (; tt < ntile; ++tt) {
-    if (w.t0 + tt * kManyTile < most) compute(tt, std::false_type{}, std::false_type{});
+  auto advance = [&]() KV8_INLINE {
     if (tt + 1 < ntile) {
       stage(tt + 1, ra);
       fetch(tt + 2, id, ra);
       id = ask(tt + 3);
-      __syncthreads();
+      __syncthreads();   // the other buffer is staged; its readers passed the last barrier
     }
+  };
+  if (any) {
+    for (; tt + 1 < nfull; ++tt) {
+      compute(tt, std::true_type{}, std::true_type{});
+      __syncthreads();   // (as above)
+    }
+    for (; tt < ntile; ++tt) {
+      if (w.t0 + tt * kManyTile < most) compute(tt, std::false_type{}, std::false_type{});
+      advance();
+    }
+  } else {
+    for (; tt < ntile; ++tt) advance();
   }
   // ---- results -----------------------------------------------------------------------
   // the own key, once
@@ -418,7 +428,7 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
       }
   }
   const float l_all = kv8_sum32(l_run);
-  auto put = [&](int d, int r, float a, float b, float e, float f) {   // four dims of the lane's column
+  auto put = [&](int d, int r, float a, float b, float e, float f) KV8_INLINE {   // four dims of the lane's column
     const int64_t to = (int64_t)row * A.out_row + (int64_t)head * A.out_head + 32 * d + 8 * (r >> 2) + 4 * hi;
     if constexpr (BF) *(u32x2_t*)((uint16_t*)A.out + to) = u32x2_t{kv8_pk(a, b), kv8_pk(e, f)};
     else *(float4*)((float*)A.out + to) = make_float4(a, b, e, f);
@@ -461,14 +471,15 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
     for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
   for (int x = 0; x < w.splits; ++x) {
     const float* p = part + (int64_t)x * pstep;
-    const float lx = ld_agent(p + ml + 1), y = kv8_weight(ld_agent(p + ml), lx, M);
+    const float2 t = ld_agent2(p + ml);
     float2 v[NO][8];
 #pragma unroll
     for (int d = 0; d < NO; ++d)
 #pragma unroll
       for (int r = 0; r < 8; ++r) v[d][r] = ld_agent2(p + mine + ((4 * d + (r >> 1)) * 64 + lane) * 4 + 2 * (r & 1));
-    if (lx != 0.f) {
-      l += y * lx;
+    const float y = kv8_weight(t.x, t.y, M);
+    if (t.y != 0.f) {
+      l += y * t.y;
 #pragma unroll
       for (int d = 0; d < NO; ++d)
 #pragma unroll
@@ -485,5 +496,7 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
     for (int r = 0; r < 16; r += 4)
       put(d, r, kv8_over(acc[d][r], l), kv8_over(acc[d][r + 1], l), kv8_over(acc[d][r + 2], l), kv8_over(acc[d][r + 3], l));
 }
+
+#undef KV8_INLINE
 
 }  // namespace m2r2
