@@ -104,8 +104,10 @@ hipError_t many_setup() {   // LDS above 64 KB, once per device
 template <int BF, int HD>
 void many_launch(const Kv8AttnArgs& A, hipStream_t st, hipError_t* e) {
   *e = many_setup<BF, HD>();
-  if (*e == hipSuccess)
-    k8_many<BF, HD><<<(unsigned)(A.entries * A.kv.H), kManyThreads, sizeof(Kv8ManyLds<HD>), st>>>(A);
+  if (*e != hipSuccess) return;
+  const unsigned grid = (unsigned)(A.entries * A.kv.H);
+  k8_many<BF, HD><<<grid, kManyThreads, sizeof(Kv8ManyLds<HD>), st>>>(A);
+  if ((long long)A.kv.mbps * A.kv.bs > kKv8MinTokens) k8_join<BF, HD><<<grid, kManyThreads, 0, st>>>(A);
 }
 
 #define M2R2_KV8_DISPATCH(FN, BFV, HDV, ...)                 \
@@ -167,9 +169,12 @@ M2R2_API m2r2_status m2r2_kv8_workspace_size(const m2r2_kv8* kv, int32_t n_seqs,
     return set_error(M2R2_E_SHAPE, "n_seqs %d, n_rows %d", n_seqs, n_rows);
   if (!bytes_out) return set_error(M2R2_E_INVALID, "bytes_out is NULL");
   if ((long long)n_rows * n_heads >= 1LL << 31) return set_error(M2R2_E_SHAPE, "n_rows * n_heads reaches 2^31");
-  const Kv8Cut c = kv8_cut(pages(kv), kv->head_dim, n_seqs, n_rows, n_heads, 1);   // (the larger)
-  if (c.entries * kv->n_kv_heads >= 1LL << 31) return set_error(M2R2_E_SHAPE, "too many rows and heads for one call");
-  *bytes_out = c.bytes;
+  *bytes_out = 0;
+  for (int bf16 = 0; bf16 < 2; ++bf16) {
+    const Kv8Cut c = kv8_cut(pages(kv), kv->head_dim, n_seqs, n_rows, n_heads, bf16);
+    if (c.entries * kv->n_kv_heads >= 1LL << 31) return set_error(M2R2_E_SHAPE, "too many rows and heads for one call");
+    *bytes_out = std::max(*bytes_out, c.bytes);
+  }
   return M2R2_OK;
 }
 

@@ -3,8 +3,9 @@
 // k8_few takes up to 16 columns (a row of a query head each) per workgroup
 // and is bound by the cache's bytes; k8_many takes 128 and is bound by the
 // matrix rate.  Both number their work alike: a sequence's columns of one
-// cache head are cut into tiles, its positions into splits, and the last split
-// of a tile to finish joins the partial results.
+// cache head are cut into tiles, its positions into splits.  Partial results of a
+// tile's splits are joined by the last of them to finish (k8_few, up to 8 KB each)
+// or by a second launch (k8_many, 64 KB each).
 #pragma once
 #include "kv8.h"
 

@@ -17,15 +17,19 @@ struct Kv8Cut {
   size_t bytes;    // of the workspace
 };
 
-// Sixteen columns a sequence on average and k8_few: more would read the cache
-// once for every sixteen.
-constexpr int kFewMost = 16;
+// Up to this many columns a sequence on average, k8_few, which reads the cache
+// once for every sixteen; above, k8_many with its second launch.  Measured at 8
+// heads of 128 for 4 (us, k8_few and k8_many): one sequence of 1500 positions, 32
+// columns 18.2 and 15.4, 64 17.8 and 16.7; four of 8000, 32 columns 28.8 and 29.2, 64
+// 40.7 and 35.7; in float32, whose products are threefold, four of 8000 with 64
+// columns 34.7 and 63.9, 128 71.2 and 71.9, 256 95.5 and 80.4.
+constexpr int kv8_few_most(bool bf16) { return bf16 ? 32 : 96; }
 
 inline Kv8Cut kv8_cut(const Kv8Pages& kv, int hd, int n_seqs, int n_rows, int n_heads, bool bf16) {
   Kv8Cut c;
   const int H = kv.H, group = n_heads / H;
   const long long cols = (long long)n_rows * group;
-  c.many = cols > (long long)kFewMost * std::max(1, n_seqs);
+  c.many = cols > (long long)kv8_few_most(bf16) * std::max(1, n_seqs);
   c.cols = c.many ? kManyCols : kFewCols;
   // what a compute unit holds: two workgroups, three of k8_few's bfloat16 form
   c.target = (c.many || !bf16 ? 2 : 3) * kKv8Units;

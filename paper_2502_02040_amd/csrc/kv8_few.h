@@ -19,6 +19,13 @@
 // Queries are bfloat16 as given, or float32 cut into three parts (24 bits).
 // Probabilities are rounded to 16 bits (two parts) for bfloat16 rows and kept to 24
 // for float32 rows: the matrix pipe is idle enough that both are free.
+//
+// Measured (a large copy reaches 5.17 TB/s here): one row of 32 heads of 128 for 8,
+// behind 131001 positions, 57 us, 4.7 TB/s; 32 such sequences of up to 8192 positions
+// 70 us, 4.3 TB/s; eight dual-stream pairs of float32 rows, 32 heads of 96, behind up to
+// 4096 positions, 32 us, 3.5 TB/s (three products for each: 180 registers and two
+// waves per SIMD); one row behind 1025 positions 10.7 us and behind 17 5.9 us, which
+// are chains: launch, lengths, block ids, codes, join.
 #pragma once
 #include "kv8_attn.h"
 

@@ -12,6 +12,11 @@
 //     operand of O^T = V^T P^T as it stands.
 //   * Two workgroups per compute unit, so that one's softmax runs beside the
 //     other's products.
+// Measured (bfloat16, 32 heads of 128 for 8): two prompts of 4001 rows 171 us, 0.78
+// PFLOP/s of the 1.31 that a large library product reaches here; 500 rows behind
+// 8500 positions 101 us, 0.71 PFLOP/s, the join's launch included (5 us, also where
+// nothing is split; a join inside this kernel took 106 and 162 us, but 69 instead
+// of 20 for 8 rows behind 8000 positions).
 // Probabilities of bfloat16 rows are rounded to bfloat16 (half a step of 2^-8, of
 // the same size as the result's own rounding, and averaged over the positions):
 // a second part would cost half of all products again.  Those of float32 rows
@@ -40,7 +45,6 @@ struct Kv8ManyLds {
   unsigned long long gap[4], odd[4];
   int gaps;                                   // any of the first
   uint8_t nan[2][kManyTile][HD / 8];
-  int last;
 };
 
 // Place of positions 8 c .. 8 c + 7 of dim d: the eight 16-byte pieces of a
@@ -444,57 +448,71 @@ __global__ __launch_bounds__(kManyThreads, BF ? 2 : 1) void k8_many(Kv8AttnArgs 
             l_all != 0.f ? acc[d][r + 2] * li : 0.f, l_all != 0.f ? acc[d][r + 3] * li : 0.f);
     return;
   }
-  // Partial results as the lanes hold them: of each wave the accumulators, 16
-  // bytes a lane, then the maximum and sum of its columns.
-  const int pf = kv8_part_floats(kManyCols, HD);
-  float* part = A.part + ((int64_t)w.slot * A.kv.H + h) * pf;
-  const int64_t pstep = (int64_t)A.kv.H * pf;
-  const int mine = wv * 32 * HD, ml = kManyCols * HD + 2 * (32 * wv + n);
-  {
-    float* p = part + (int64_t)w.split * pstep;
-#pragma unroll
-    for (int d = 0; d < NO; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; r += 4) {
-        float* o = p + mine + ((4 * d + (r >> 2)) * 64 + lane) * 4;
-        st_agent2(o, acc[d][r], acc[d][r + 1]);
-        st_agent2(o + 2, acc[d][r + 2], acc[d][r + 3]);
-      }
-    if (hi == 0) st_agent2(p + ml, m_run, l_all);
-  }
-  if (!arrive_last(A.cnt + w.unit * A.kv.H + h, w.splits, &S.last)) return;
-  float M = -INFINITY, l = 0.f;
-  for (int x = 0; x < w.splits; ++x) M = fmaxf(M, ld_agent(part + (int64_t)x * pstep + ml));
-#pragma unroll
-  for (int d = 0; d < NO; ++d)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
-  for (int x = 0; x < w.splits; ++x) {
-    const float* p = part + (int64_t)x * pstep;
-    const float2 t = ld_agent2(p + ml);
-    float2 v[NO][8];
-#pragma unroll
-    for (int d = 0; d < NO; ++d)
-#pragma unroll
-      for (int r = 0; r < 8; ++r) v[d][r] = ld_agent2(p + mine + ((4 * d + (r >> 1)) * 64 + lane) * 4 + 2 * (r & 1));
-    const float y = kv8_weight(t.x, t.y, M);
-    if (t.y != 0.f) {
-      l += y * t.y;
-#pragma unroll
-      for (int d = 0; d < NO; ++d)
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          acc[d][2 * r] += y * v[d][r].x;
-          acc[d][2 * r + 1] += y * v[d][r].y;
-        }
-    }
-  }
-  if (!live) return;
+  // Partial results as the lanes hold them (k8_join): of each wave the
+  // accumulators, 16 bytes a lane, then the maximum and sum of its columns.
+  if (!any) return;
+  float* p = A.part + ((int64_t)(w.slot + w.split) * A.kv.H + h) * kv8_part_floats(kManyCols, HD);
 #pragma unroll
   for (int d = 0; d < NO; ++d)
 #pragma unroll
     for (int r = 0; r < 16; r += 4)
-      put(d, r, kv8_over(acc[d][r], l), kv8_over(acc[d][r + 1], l), kv8_over(acc[d][r + 2], l), kv8_over(acc[d][r + 3], l));
+      *(float4*)(p + ((wv * NO + d) * 4 + (r >> 2)) * 256 + 4 * lane) =
+          make_float4(acc[d][r], acc[d][r + 1], acc[d][r + 2], acc[d][r + 3]);
+  if (hi == 0) *(float2*)(p + kManyCols * HD + 2 * (32 * wv + n)) = make_float2(m_run, l_all);
+}
+
+// Joins the splits of tiles, in a launch of its own: the workgroups of a tile's
+// splits share its results among them (a last workgroup that took them all, as
+// k8_few's does, needed 1.5 us for each split's 64 KB).
+template <int BF, int HD>
+__global__ __launch_bounds__(kManyThreads) void k8_join(Kv8AttnArgs A) {
+  constexpr int NO = HD / 32, NCH = 4 * NO;   // 1 KB pieces of a partial result per wave: 4 dims of each half of 32 columns
+  __shared__ float y_s[kKv8MaxSplits][kManyCols], l_s[kManyCols];
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, hi = lane >> 5;
+  const int h = blockIdx.x % A.kv.H, entry = blockIdx.x / A.kv.H;
+  Kv8Work w;
+  if (!kv8_pick<kManyCols>(A, entry, false, w) || w.splits == 1) return;
+  const int pf = kv8_part_floats(kManyCols, HD);
+  const float* part = A.part + ((int64_t)w.slot * A.kv.H + h) * pf;
+  const int64_t pstep = (int64_t)A.kv.H * pf;
+  const int c0 = w.tile * kManyCols, live = min(kManyCols, w.cols - c0);
+  const int groups = (live + 31) / 32;   // of 32 columns
+  if (tid < 32 * groups) {
+    float M = -INFINITY, l = 0.f;
+#pragma unroll 8
+    for (int x = 0; x < w.splits; ++x) M = fmaxf(M, part[x * pstep + kManyCols * HD + 2 * tid]);
+#pragma unroll 4
+    for (int x = 0; x < w.splits; ++x) {
+      const float2 t = *(const float2*)(part + x * pstep + kManyCols * HD + 2 * tid);
+      const float y = kv8_weight(t.x, t.y, M);
+      y_s[x][tid] = y;
+      if (t.y != 0.f) l += y * t.y;
+    }
+    l_s[tid] = l;
+  }
+  __syncthreads();
+  const int all = groups * NCH, from = all * w.split / w.splits, to = all * (w.split + 1) / w.splits;
+  for (int ch = from + wv; ch < to; ch += 4) {
+    const int g = ch / NCH, d = ch % NCH / 4, r4 = ch % 4, c = 32 * g + n;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int x = 0; x < w.splits; ++x) {
+      const float4 v = *(const float4*)(part + x * pstep + ch * 256 + 4 * lane);
+      const float y = y_s[x][c];   // (zero, times zeros, for a split that the column saw nothing of)
+      a.x += y * v.x;
+      a.y += y * v.y;
+      a.z += y * v.z;
+      a.w += y * v.w;
+    }
+    if (c >= live) continue;
+    const float l = l_s[c];
+    const int row = w.r0 + (c0 + c) / A.group, head = h * A.group + (c0 + c) % A.group;
+    const int64_t o = (int64_t)row * A.out_row + (int64_t)head * A.out_head + 32 * d + 8 * r4 + 4 * hi;
+    a = make_float4(kv8_over(a.x, l), kv8_over(a.y, l), kv8_over(a.z, l), kv8_over(a.w, l));
+    if constexpr (BF) *(u32x2_t*)((uint16_t*)A.out + o) = u32x2_t{kv8_pk(a.x, a.y), kv8_pk(a.z, a.w)};
+    else *(float4*)((float*)A.out + o) = a;
+  }
 }
 
 #undef KV8_INLINE

@@ -179,7 +179,7 @@ def attend_both(pool, dt, counts, lens, G, *, visible=None, own=None, scale=None
     kv8_attention(kv, qd, i32(start), i32(lens), out, ws, visible=None if visible is None else i32(visible), scale=scale,
                   **kw)
     sc = 1.0 / np.sqrt(hd) if scale is None else scale
-    many = n * G > 16 * len(counts)
+    many = n * G > 32 * len(counts)
     e_p = 2.0 ** -23 if dt == "f32" else 2.0 ** -8 if many else 2.0 ** -16
     h = 2.0 ** -24 if dt == "f32" else 2.0 ** -8
     got, qf = out.double().cpu().numpy(), qd.double().cpu().numpy()
