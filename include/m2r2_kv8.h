@@ -52,7 +52,8 @@ typedef struct {
  * row_start_d[s+1]-1 of the call's n_rows.  Rows that belong to no sequence
  * (behind the last one of a padded batch) are neither read nor written.
  * Element (row, head, dim) of an array lies at row * row_stride + head *
- * head_stride + dim elements; every (row, head) starts on 16 bytes. */
+ * head_stride + dim elements; every (row, head) starts on 16 bytes.  Arrays
+ * without rows, and per-sequence arrays without sequences, may be NULL. */
 typedef struct {
   int32_t n_seqs, n_rows;
   const int32_t* row_start_d;    /* [n_seqs + 1], ascending from row_start_d[0] >= 0 to at most n_rows */
@@ -86,8 +87,10 @@ typedef struct {
  *
  * Two sequences must not append to the same physical block in one call (two
  * that share a prefix share only whole blocks): what such a block then holds
- * is one's rows, the other's, or a mixture.  The arrays must not overlap the
- * cache. */
+ * is one's rows, the other's, or a mixture.  The same holds for a table that
+ * names a block twice among those that one sequence appends to.  The arrays
+ * must not overlap each other (but q_out q) or the cache; in q_out neither rows
+ * nor heads overlap, in the others both strides may be 0. */
 M2R2_API m2r2_status m2r2_kv8_append(const m2r2_kv8* kv, const m2r2_kv8_rows* rows, hipStream_t stream);
 
 typedef struct {
@@ -121,8 +124,9 @@ M2R2_API m2r2_status m2r2_kv8_workspace_size(const m2r2_kv8* kv, int32_t n_seqs,
                                              size_t* bytes_out);
 
 /* out = softmax(scale * q K^T) V over the positions that each row sees and
- * its own key and value, if it has one.  A row that sees nothing is zero.  What a row does not see does
- * not reach it, NaN included.  Scores, the softmax and all sums are float32.
+ * its own key and value, if it has one.  A row that sees nothing is zero.  What
+ * a row does not see does not reach it, NaN included.  Scores, the softmax and
+ * all sums are float32.  `out` overlaps none of the other arrays and the cache.
  *
  * `workspace`: device memory of at least m2r2_kv8_workspace_size() bytes, 256-byte
  * aligned, zeroed by the caller before its first use; every call leaves it

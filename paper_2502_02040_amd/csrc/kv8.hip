@@ -18,8 +18,8 @@ namespace {
 
 bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
-m2r2_status check_pages(const m2r2_kv8* kv) {
-  if (!kv || !kv->k_pages || !kv->v_pages || !kv->k_scales || !kv->v_scales || !kv->block_table_d)
+m2r2_status check_pages(const m2r2_kv8* kv, int32_t n_seqs) {
+  if (!kv || !kv->k_pages || !kv->v_pages || !kv->k_scales || !kv->v_scales || (!kv->block_table_d && n_seqs))
     return set_error(M2R2_E_INVALID, "kv descriptor or one of its pointers is NULL");
   if (!aligned(kv->k_pages, 16) || !aligned(kv->v_pages, 16))
     return set_error(M2R2_E_INVALID, "kv pages not 16-byte aligned");
@@ -40,21 +40,40 @@ m2r2_status check_pages(const m2r2_kv8* kv) {
   return M2R2_OK;
 }
 
-m2r2_status check_rows(int32_t n_seqs, int32_t n_rows, const int32_t* row_start, int32_t dtype) {
+m2r2_status check_counts(int32_t n_seqs, int32_t n_rows) {
   if (n_seqs < 0 || n_rows < 0 || n_seqs > 1 << 20 || n_rows > 1 << 26)
     return set_error(M2R2_E_SHAPE, "n_seqs %d, n_rows %d", n_seqs, n_rows);
+  return M2R2_OK;
+}
+
+m2r2_status check_rows(int32_t n_seqs, int32_t n_rows, const int32_t* row_start, int32_t dtype) {
+  if (m2r2_status s = check_counts(n_seqs, n_rows)) return s;
   if (!row_start || !aligned(row_start, 4)) return set_error(M2R2_E_INVALID, "row_start_d NULL or misaligned");
   if (dtype != M2R2_F32 && dtype != M2R2_BF16) return set_error(M2R2_E_DTYPE, "dtype %d", dtype);
   return M2R2_OK;
 }
 
-m2r2_status check_array(const char* name, const void* p, int64_t row, int64_t head, int32_t dtype) {
+// (the stride of a dimension of one entry does not count)
+m2r2_status check_array(const char* name, const void* p, int n, int heads, int64_t row, int64_t head, int32_t dtype) {
+  if (!n) return M2R2_OK;
   if (!p) return set_error(M2R2_E_INVALID, "%s is NULL", name);
   const int64_t per = dtype == M2R2_BF16 ? 8 : 4;
-  if (!aligned(p, 16) || row % per || head % per)
+  if (!aligned(p, 16) || (n > 1 && row % per) || (heads > 1 && head % per))
     return set_error(M2R2_E_INVALID, "%s: a row or head does not start on 16 bytes", name);
-  if (row < 0 || head < 0) return set_error(M2R2_E_SHAPE, "%s: negative stride", name);
+  const int64_t most = 1LL << 36;
+  if ((n > 1 && (row < 0 || row > most)) || (heads > 1 && (head < 0 || head > most)))
+    return set_error(M2R2_E_SHAPE, "%s: stride negative or above 2^36", name);
   return M2R2_OK;
+}
+
+// One that is written: its rows of heads, or its heads of rows, lie apart.
+m2r2_status check_written(const char* name, const void* p, int n, int heads, int64_t row, int64_t head, int hd,
+                          int32_t dtype) {
+  if (m2r2_status s = check_array(name, p, n, heads, row, head, dtype)) return s;
+  if (!n) return M2R2_OK;
+  const bool by_row = (heads < 2 || head >= hd) && (n < 2 || row >= (heads < 2 ? 0 : (heads - 1) * head) + hd);
+  const bool by_head = (n < 2 || row >= hd) && (heads < 2 || head >= (n < 2 ? 0 : (n - 1) * row) + hd);
+  return by_row || by_head ? M2R2_OK : set_error(M2R2_E_INVALID, "%s: rows and heads overlap", name);
 }
 
 m2r2_status check_heads(const m2r2_kv8* kv, int32_t n_heads) {
@@ -87,6 +106,8 @@ void few_launch(const Kv8AttnArgs& A, hipStream_t st) {
   k8_few<BF, HD><<<(unsigned)(A.entries * A.kv.H), kFewThreads, 0, st>>>(A, Kv8Out<BF, HD>{});
 }
 
+// A launch has fewer than 2^32 threads along x.
+constexpr long long kMaxGrid = 1 << 24;
 constexpr int kMaxDevices = 64;
 
 template <int BF, int HD>
@@ -128,19 +149,20 @@ void many_launch(const Kv8AttnArgs& A, hipStream_t st, hipError_t* e) {
 extern "C" {
 
 M2R2_API m2r2_status m2r2_kv8_append(const m2r2_kv8* kv, const m2r2_kv8_rows* r, hipStream_t stream) {
-  if (m2r2_status s = check_pages(kv)) return s;
   if (!r) return set_error(M2R2_E_INVALID, "rows descriptor is NULL");
+  if (m2r2_status s = check_pages(kv, r->n_seqs)) return s;
   if (m2r2_status s = check_rows(r->n_seqs, r->n_rows, r->row_start_d, r->dtype)) return s;
-  if (!r->positions_d || !aligned(r->positions_d, 4)) return set_error(M2R2_E_INVALID, "positions_d NULL or misaligned");
-  if (m2r2_status s = check_array("k", r->k, r->k_row, r->k_head, r->dtype)) return s;
-  if (m2r2_status s = check_array("v", r->v, r->v_row, r->v_head, r->dtype)) return s;
+  if ((!r->positions_d && r->n_seqs) || !aligned(r->positions_d, 4)) return set_error(M2R2_E_INVALID, "positions_d NULL or misaligned");
+  if (m2r2_status s = check_array("k", r->k, r->n_rows, kv->n_kv_heads, r->k_row, r->k_head, r->dtype)) return s;
+  if (m2r2_status s = check_array("v", r->v, r->n_rows, kv->n_kv_heads, r->v_row, r->v_head, r->dtype)) return s;
   if (r->rope_d && (!aligned(r->rope_d, 16) || r->rope_len < 1))
     return set_error(M2R2_E_INVALID, "rope_d not 16-byte aligned, or rope_len %d", r->rope_len);
   if (r->n_heads) {
     if (m2r2_status s = check_heads(kv, r->n_heads)) return s;
-    if (m2r2_status s = check_array("q", r->q, r->q_row, r->q_head, r->dtype)) return s;
-    if (m2r2_status s = check_array("q_out", r->q_out, r->qo_row, r->qo_head, r->dtype)) return s;
-    if (r->q == r->q_out && (r->q_row != r->qo_row || r->q_head != r->qo_head))
+    if (m2r2_status s = check_array("q", r->q, r->n_rows, r->n_heads, r->q_row, r->q_head, r->dtype)) return s;
+    if (m2r2_status s = check_written("q_out", r->q_out, r->n_rows, r->n_heads, r->qo_row, r->qo_head, kv->head_dim, r->dtype))
+      return s;
+    if (r->q == r->q_out && ((r->n_rows > 1 && r->q_row != r->qo_row) || (r->n_heads > 1 && r->q_head != r->qo_head)))
       return set_error(M2R2_E_INVALID, "q_out is q with other strides");
   } else if (r->q || r->q_out) {
     return set_error(M2R2_E_INVALID, "q or q_out given with n_heads 0");
@@ -155,7 +177,7 @@ M2R2_API m2r2_status m2r2_kv8_append(const m2r2_kv8* kv, const m2r2_kv8_rows* r,
   A.rope = r->rope_d; A.rope_len = r->rope_len; A.n_heads = r->n_heads; A.err = r->err_d;
   A.units = kv->n_kv_heads + (r->n_heads + kKv8QHeads - 1) / kKv8QHeads;
   if (!r->n_seqs || !r->n_rows) return M2R2_OK;
-  if ((long long)kv8_block_base(r->n_rows, r->n_seqs, kv->block_size) * A.units >= 1LL << 31)
+  if ((long long)kv8_block_base(r->n_rows, r->n_seqs, kv->block_size) * A.units >= kMaxGrid)
     return set_error(M2R2_E_SHAPE, "too many rows and heads for one call");
   M2R2_KV8_DISPATCH(append_launch, r->dtype == M2R2_BF16, kv->head_dim, A, stream);
   return launched("m2r2_kv8_append");
@@ -163,16 +185,15 @@ M2R2_API m2r2_status m2r2_kv8_append(const m2r2_kv8* kv, const m2r2_kv8_rows* r,
 
 M2R2_API m2r2_status m2r2_kv8_workspace_size(const m2r2_kv8* kv, int32_t n_seqs, int32_t n_rows, int32_t n_heads,
                                              size_t* bytes_out) {
-  if (m2r2_status s = check_pages(kv)) return s;
+  if (m2r2_status s = check_counts(n_seqs, n_rows)) return s;
+  if (m2r2_status s = check_pages(kv, n_seqs)) return s;
   if (m2r2_status s = check_heads(kv, n_heads)) return s;
-  if (n_seqs < 0 || n_rows < 0 || n_seqs > 1 << 20 || n_rows > 1 << 26)
-    return set_error(M2R2_E_SHAPE, "n_seqs %d, n_rows %d", n_seqs, n_rows);
   if (!bytes_out) return set_error(M2R2_E_INVALID, "bytes_out is NULL");
   if ((long long)n_rows * n_heads >= 1LL << 31) return set_error(M2R2_E_SHAPE, "n_rows * n_heads reaches 2^31");
   *bytes_out = 0;
   for (int bf16 = 0; bf16 < 2; ++bf16) {
     const Kv8Cut c = kv8_cut(pages(kv), kv->head_dim, n_seqs, n_rows, n_heads, bf16);
-    if (c.entries * kv->n_kv_heads >= 1LL << 31) return set_error(M2R2_E_SHAPE, "too many rows and heads for one call");
+    if (c.entries * kv->n_kv_heads >= kMaxGrid) return set_error(M2R2_E_SHAPE, "too many rows and heads for one call");
     *bytes_out = std::max(*bytes_out, c.bytes);
   }
   return M2R2_OK;
@@ -180,23 +201,24 @@ M2R2_API m2r2_status m2r2_kv8_workspace_size(const m2r2_kv8* kv, int32_t n_seqs,
 
 M2R2_API m2r2_status m2r2_kv8_attention(const m2r2_kv8* kv, const m2r2_kv8_query* a, void* workspace, size_t ws_bytes,
                                         hipStream_t stream) {
-  if (m2r2_status s = check_pages(kv)) return s;
   if (!a) return set_error(M2R2_E_INVALID, "query descriptor is NULL");
+  if (m2r2_status s = check_pages(kv, a->n_seqs)) return s;
   if (m2r2_status s = check_rows(a->n_seqs, a->n_rows, a->row_start_d, a->dtype)) return s;
-  if (!a->lens_d || !aligned(a->lens_d, 4)) return set_error(M2R2_E_INVALID, "lens_d NULL or misaligned");
+  if ((!a->lens_d && a->n_seqs) || !aligned(a->lens_d, 4)) return set_error(M2R2_E_INVALID, "lens_d NULL or misaligned");
   if (!aligned(a->visible_d, 4) || !aligned(a->own_d, 4) || !aligned(a->err_d, 4))
     return set_error(M2R2_E_INVALID, "visible_d, own_d or err_d misaligned");
   if (m2r2_status s = check_heads(kv, a->n_heads)) return s;
-  if (m2r2_status s = check_array("q", a->q, a->q_row, a->q_head, a->dtype)) return s;
-  if (m2r2_status s = check_array("out", a->out, a->out_row, a->out_head, a->dtype)) return s;
-  if (a->own_d) {
-    if (a->n_own < 1) return set_error(M2R2_E_SHAPE, "n_own %d", a->n_own);
-    if (m2r2_status s = check_array("own_k", a->own_k, a->ok_row, a->ok_head, a->dtype)) return s;
-    if (m2r2_status s = check_array("own_v", a->own_v, a->ov_row, a->ov_head, a->dtype)) return s;
-  }
-  if (!(a->scale >= 0.f) || a->scale > 3e38f) return set_error(M2R2_E_INVALID, "scale");
   size_t need = 0;
   if (m2r2_status s = m2r2_kv8_workspace_size(kv, a->n_seqs, a->n_rows, a->n_heads, &need)) return s;
+  if (m2r2_status s = check_array("q", a->q, a->n_rows, a->n_heads, a->q_row, a->q_head, a->dtype)) return s;
+  if (m2r2_status s = check_written("out", a->out, a->n_rows, a->n_heads, a->out_row, a->out_head, kv->head_dim, a->dtype))
+    return s;
+  if (a->own_d) {
+    if (a->n_own < 1) return set_error(M2R2_E_SHAPE, "n_own %d", a->n_own);
+    if (m2r2_status s = check_array("own_k", a->own_k, a->n_own, kv->n_kv_heads, a->ok_row, a->ok_head, a->dtype)) return s;
+    if (m2r2_status s = check_array("own_v", a->own_v, a->n_own, kv->n_kv_heads, a->ov_row, a->ov_head, a->dtype)) return s;
+  }
+  if (!(a->scale >= 0.f) || a->scale > 3e38f) return set_error(M2R2_E_INVALID, "scale");
   if (!workspace || !aligned(workspace, 256)) return set_error(M2R2_E_INVALID, "workspace NULL or not 256-byte aligned");
   if (ws_bytes < need) return set_error(M2R2_E_NOMEM, "workspace of %zu bytes, %zu needed", ws_bytes, need);
   if (!a->n_seqs || !a->n_rows) return M2R2_OK;

@@ -179,7 +179,9 @@ __device__ __forceinline__ bool kv8_pick(const Kv8AttnArgs& A, int entry, bool r
     }
     const int p = max(per, ((len + A.max_splits - 1) / A.max_splits + 63) / 64 * 64);
     const int splits = max(1, (len + p - 1) / p);
-    const int mine = tiles * splits, ms = splits > 1 ? mine : 0, mu = splits > 1 ? tiles : 0;
+    // (row starts out of order can name rows many times over: capped, so that the
+    // counts below stay in range until they are found to exceed the grid)
+    const int mine = min(tiles * splits, A.entries + 1), ms = splits > 1 ? mine : 0, mu = splits > 1 ? tiles : 0;
     const int upto = kv8_wave_scan(mine), us = kv8_wave_scan(ms), uu = kv8_wave_scan(mu);
     const uint64_t hit = __ballot(entry >= before + upto - mine && entry < before + upto);
     if (hit) {
@@ -199,9 +201,9 @@ __device__ __forceinline__ bool kv8_pick(const Kv8AttnArgs& A, int entry, bool r
       w.slot = slots + of(us - ms) + w.tile * w.splits;
       w.unit = units + of(uu - mu) + w.tile;
     }
-    before += __builtin_amdgcn_readlane(upto, 63);
-    slots += __builtin_amdgcn_readlane(us, 63);
-    units += __builtin_amdgcn_readlane(uu, 63);
+    before = min(before + __builtin_amdgcn_readlane(upto, 63), 1 << 30);
+    slots = min(slots + __builtin_amdgcn_readlane(us, 63), 1 << 30);
+    units = min(units + __builtin_amdgcn_readlane(uu, 63), 1 << 30);
   }
   // row starts that overlap can ask for more than the grid holds: nothing is done then
   if (before > A.entries) {

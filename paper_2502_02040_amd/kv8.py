@@ -157,13 +157,13 @@ def kv8_append(kv: KV8Pages, k, v, row_start, positions, *, rope=None, q=None, q
     ``rope`` [length][head_dim/2][2] float32 (cos, sin) turns the keys (and the
     queries ``q`` [rows][heads][head_dim] into ``q_out``, which may be ``q``).
     ``errors``: an int32 tensor into which the kernels or error bits."""
-    n, H, hd, ns, gpu = k.shape[0], kv.n_kv_heads, kv.head_dim, kv.n_seqs, kv.gpu
+    n, H, hd, ns, gpu = len(k), kv.n_kv_heads, kv.head_dim, kv.n_seqs, kv.gpu
     code, dt = _dtype(k, "k")
     kp, k_row, k_head = _rows(k, "k", n, H, hd, dt, gpu)
     vp, v_row, v_head = _rows(v, "v", n, H, hd, dt, gpu)
     heads, qp, q_row, q_head, op, o_row, o_head = 0, None, 0, 0, None, 0, 0
     if q is not None and q_out is not None:
-        heads = q.shape[1]
+        heads = q.shape[1] if q.dim() == 3 else 0
         qp, q_row, q_head = _rows(q, "q", n, heads, hd, dt, gpu)
         op, o_row, o_head = _rows(q_out, "q_out", n, heads, hd, dt, gpu)
     elif q is not None or q_out is not None:
@@ -197,15 +197,22 @@ def kv8_attention(kv: KV8Pages, q, row_start, lens, out, workspace, *, visible=N
     min(visible[r], lens[s]) of them (None: causal, the sequence's last row sees
     all) and, where own[r] >= 0, the key and value own_k/own_v[own[r]] beside
     them.  A row that sees nothing is zero."""
+    if q.dim() != 3:
+        raise ValueError(f"q: {tuple(q.shape)}; expected [rows][heads][head_dim]")
     n, heads, H, hd, ns, gpu = q.shape[0], q.shape[1], kv.n_kv_heads, kv.head_dim, kv.n_seqs, kv.gpu
+    if scale is not None and not scale > 0:
+        raise ValueError(f"scale {scale}")
     code, dt = _dtype(q, "q")
     qp, q_row, q_head = _rows(q, "q", n, heads, hd, dt, gpu)
     op, o_row, o_head = _rows(out, "out", n, heads, hd, dt, gpu)
     n_own, kp, k_row, k_head, vp, v_row, v_head = 0, None, 0, 0, None, 0, 0
-    if own is not None:
+    if own is not None and own_k is not None and own_v is not None:
         n_own = own_k.shape[0]
         kp, k_row, k_head = _rows(own_k, "own_k", n_own, H, hd, dt, gpu)
         vp, v_row, v_head = _rows(own_v, "own_v", n_own, H, hd, dt, gpu)
+        own = own if n_own else None
+    elif own is not None or own_k is not None or own_v is not None:
+        raise ValueError("own, own_k and own_v come together")
     if workspace.get_device() != gpu or not workspace.is_contiguous():
         raise ValueError(f"workspace: a contiguous tensor on GPU {gpu}")
     a = _Query(ns, n, _int32s(row_start, ns + 1, "row_start", gpu), _int32s(lens, ns, "lens", gpu),

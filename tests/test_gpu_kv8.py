@@ -9,6 +9,10 @@ worst-case arithmetic (u = 2^-24, half a step of float32):
   sums     of n positions and the joins: 2 u (n + 128)
 so |out - ref| <= vmax (2 |dz| + e_p + 2 u (n + 128)) + h |ref|, h half a step of the result's type.
 """
+import pathlib
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -422,3 +426,86 @@ def test_decoding_together_captured_and_replayed():
         assert torch.equal(kv.k_pages.view(torch.uint8), other.k_pages.view(torch.uint8))
         assert torch.equal(kv.v_scales, other.v_scales)
     assert p2.tolist() == [L + 21 for L in lens0] and pos.tolist() == p2.tolist()
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_broadcast_rows_and_empty_batches(n):
+    """Both strides 0: every row and head reads the same vector; and empty batches enqueue nothing."""
+    H, hd = 2, 64
+    pool = Pool(19, 2, 4, H, hd, 16)
+    kv, ref, rng = pool.upload(), pool.ref(), pool.rng
+    x = torch.tensor(rng.standard_normal((1, 1, hd)), dtype=torch.float32, device="cuda").expand(n, H, hd)
+    start = i32([0, n // 2, n])
+    kv8_append(kv, x, x, start, i32([3, 9]))
+    for s, (c, p) in enumerate(((n // 2, 3), (n - n // 2, 9))):
+        if c:
+            for which in range(2):
+                ref.append(which, pool.table[s], p, np.broadcast_to(x[0].cpu().numpy(), (c, H, hd)))
+    same_cache(kv, ref)
+    none = torch.empty(0, H, hd, device="cuda")
+    kv8_append(kv, none, none, i32([0, 0, 0]), i32([3, 9]), q=none, q_out=none)
+    kv8_attention(kv, none, i32([0, 0, 0]), i32([3, 9]), none, kv8_workspace(kv, none))
+    q, out = torch.randn(n, H, hd, device="cuda"), torch.zeros(n, H, hd, device="cuda")
+    kv8_attention(kv, q, start, i32([20, 50]), out, kv8_workspace(kv, q), own=i32([-1] * n), own_k=none, own_v=none)
+    same_cache(kv, ref)
+
+
+@pytest.mark.parametrize("n,dt", [(2, "bf16"), (3, "f32"), (70, "bf16"), (200, "f32")])
+def test_a_pool_beyond_32_bits(n, dt):
+    """Blocks on both sides of 2^32 bytes (and 2^31): rows appended there, then attended to."""
+    H, hd, bs, nb, L = 4, 128, 64, 140000, 1000 + n   # 32 KB a block and head set: 4.27 GiB of keys, as many of values
+    pages = [torch.empty(nb, H, bs, hd, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn) for _ in range(2)]
+    scales = [torch.ones(nb, H, device="cuda") for _ in range(2)]
+    near = [(1 << 31) // (H * bs * hd), (1 << 32) // (H * bs * hd)]
+    want = [nb - 1, 0, near[0], near[0] - 1, near[1], near[1] - 1]
+    blocks = np.array(want + [i * 8009 + 11 for i in range(-(-L // bs) - len(want))], dtype=np.int32)
+    kv = KV8Pages(*pages, *scales, i32(blocks[None]))
+    rng = np.random.default_rng(n)
+    k, v = (torch.tensor(rng.standard_normal((L, H, hd))).to(DT[dt]).cuda() for _ in range(2))
+    kv8_append(kv, k, v, i32([0, L]), i32([0]))
+    small = Pool(20, 1, len(blocks), H, hd, bs)       # the same blocks, in order, as a pool of their own
+    small.table = np.arange(len(blocks), dtype=np.int32)[None]
+    small.codes = [np.zeros((len(blocks), H, bs, hd), np.uint8) for _ in range(2)]
+    small.scales = [np.ones((len(blocks), H)) for _ in range(2)]
+    small.upload()
+    ref = small.ref()
+    for which, x in enumerate((k, v)):
+        ref.append(which, small.table[0], 0, x.float().cpu().numpy())
+    for c, s, codes, exps in zip(pages, scales, ref.codes, ref.exps):
+        got = c.view(torch.uint8)[torch.tensor(blocks, device="cuda").long()].cpu().numpy()
+        for b in range(len(blocks)):
+            m = min(bs, L - b * bs)
+            assert np.array_equal(kv8_ref.CODE[got[b, :, :m]], kv8_ref.CODE[codes[b, :, :m]]), b
+        assert np.array_equal(s[torch.tensor(blocks, device="cuda").long()].cpu().numpy(), 2.0 ** exps)
+    small.codes, small.scales, small.kv = ref.codes, [2.0 ** e for e in ref.exps], kv
+    attend_both(small, dt, [n], [L], 2)
+
+
+def test_a_first_call_in_a_capture():
+    """A program whose first call of the attention for many columns is captured: nothing of it waits for an eager one."""
+    code = """
+import torch, sys
+sys.path.insert(0, {root!r})
+from paper_2502_02040_amd import KV8Pages, kv8_attention, kv8_workspace
+z = lambda *s: torch.randint(0, 120, s, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+one = lambda: torch.ones(64, 2, device="cuda")
+kv = KV8Pages(z(64, 2, 16, 64), z(64, 2, 16, 64), one(), one(), torch.arange(64, dtype=torch.int32, device="cuda")[None].contiguous())
+q, out = torch.randn(200, 4, 64, device="cuda").bfloat16(), torch.zeros(200, 4, 64, device="cuda").bfloat16()
+start, lens = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, 200], [1000]))
+ws = kv8_workspace(kv, q)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    kv8_attention(kv, q, start, lens, out, ws)
+for _ in range(3):
+    out.zero_()
+    g.replay()
+    torch.cuda.synchronize()
+    a = out.clone()
+    kv8_attention(kv, q, start, lens, out, ws)
+    assert a.abs().sum() > 0 and torch.equal(a, out)
+print("same")
+"""
+    root = str(pathlib.Path(__file__).resolve().parent.parent)
+    r = subprocess.run([sys.executable, "-c", code.format(root=root)], capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]

@@ -87,6 +87,38 @@ def test_nothing_to_do_is_no_error():
     assert attention(_pages(), _query(n_seqs=0), P, 1 << 40, None) == 0
 
 
+def test_empty_calls_need_no_arrays():
+    """A step without rows or without sequences: torch's empty tensors have no address."""
+    append, size, attention = kv8._lib()
+    none = dict(row_start_d=P, k=None, v=None, q=None, q_out=None, n_heads=4)
+    assert append(_pages(), _rows(n_rows=0, **none), None) == 0
+    assert append(_pages(block_table_d=None), _rows(n_seqs=0, positions_d=None), None) == 0
+    assert attention(_pages(), _query(n_rows=0, q=None, out=None), P, 1 << 40, None) == 0
+    assert attention(_pages(block_table_d=None), _query(n_seqs=0, lens_d=None), P, 1 << 40, None) == 0
+    n = ctypes.c_size_t(0)
+    assert size(_pages(block_table_d=None), 0, 0, 4, n) == 0
+
+
+@pytest.mark.parametrize("bad", [dict(out_row=0), dict(out_head=0), dict(out_row=128), dict(out_head=128, out_row=256),
+                                 dict(out_row=64, out_head=128)])
+def test_overlapping_results_refused(bad):
+    assert kv8._lib()[2](_pages(), _query(**bad), P, 1 << 40, None) == -1
+    turned = {k.replace("out", "qo"): x for k, x in bad.items()}
+    d = dict(n_heads=4, q=2 * P, q_out=P, q_row=256, q_head=64, qo_row=256, qo_head=64)
+    assert kv8._lib()[0](_pages(), _rows(**{**d, **turned}), None) == -1
+
+
+def test_more_workgroups_than_a_launch_holds():
+    """n_rows and heads within their own limits, refused together (2^32 threads)."""
+    append, size, _ = kv8._lib()
+    n = ctypes.c_size_t(0)
+    big = _pages(n_kv_heads=64)
+    assert size(big, 1, 1 << 25, 64, n) == -2 and n.value == 0
+    assert append(big, _rows(n_rows=1 << 25, k_row=4096, v_row=4096), None) == -2
+    assert size(_pages(n_kv_heads=8), 1, 1 << 20, 32, n) == 0   # a million rows are not too many
+    assert append(_pages(), _rows(k_row=(1 << 36) + 8), None) == -2
+
+
 def test_workspace_grows_with_the_call():
     _, size, _ = kv8._lib()
     got = []
@@ -123,6 +155,12 @@ def test_binding_refuses_wrong_tensors():
         kv8.kv8_append(kv, row, row, start, pos, rope=torch.zeros(4, 32))
     with pytest.raises(ValueError):
         kv8.kv8_attention(kv, row, start, pos, row[:2], torch.zeros(4, dtype=torch.uint8))
+    ws, own = torch.zeros(4, dtype=torch.uint8), torch.zeros(3, **i32)
+    for kw in (dict(own=own), dict(own_k=row, own_v=row), dict(scale=0.0), dict(scale=float("nan"))):
+        with pytest.raises(ValueError):
+            kv8.kv8_attention(kv, row, start, pos, torch.zeros_like(row), ws, **kw)
+    with pytest.raises(ValueError):
+        kv8.kv8_attention(kv, row[0], start, pos, row[0], ws)
     with pytest.raises(binding.M2R2Error):
         kv8.kv8_workspace(kv, torch.zeros(2, 3, 64))
 
