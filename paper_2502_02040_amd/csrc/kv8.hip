@@ -128,7 +128,7 @@ void many_launch(const Kv8AttnArgs& A, hipStream_t st, hipError_t* e) {
   if (*e != hipSuccess) return;
   const unsigned grid = (unsigned)(A.entries * A.kv.H);
   k8_many<BF, HD><<<grid, kManyThreads, sizeof(Kv8ManyLds<HD>), st>>>(A);
-  if ((long long)A.kv.mbps * A.kv.bs > kKv8MinTokens) k8_join<BF, HD><<<grid, kManyThreads, 0, st>>>(A);
+  if ((long long)A.kv.mbps * A.kv.bs > kKv8Whole) k8_join<BF, HD><<<grid, kManyThreads, 0, st>>>(A);
 }
 
 #define M2R2_KV8_DISPATCH(FN, BFV, HDV, ...)                 \

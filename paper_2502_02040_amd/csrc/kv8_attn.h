@@ -34,6 +34,15 @@ constexpr int kKv8Units = 256;         // compute units
 constexpr int kKv8FullTokens = 512;
 constexpr int kKv8MaxSplits = 64;      // of a tile: a lane each in the join
 constexpr int kKv8MinTokens = 128;     // of a split, at least: a tile of 32 for each of four waves
+// Sequences up to this long are not split: the join's chain of waits costs more.
+// One row of 32 heads of 96, whole and in splits of 128 (us): 130 positions 6.8 and
+// 9.1, 400 8.4 and 9.2, 520 9.0 and 9.4, 700 9.7 and 9.6, 1025 11.9 and 10.7.
+constexpr int kKv8Whole = 512;
+// Nor are they where k8_many would cut a tile into two or three and save less than
+// this: workgroups that share a compute unit gain little, and its join is a launch.
+// Rows of 32 heads for 8, whole and split: 400 behind 300 positions 26.7 and 33.7, 400
+// behind 600 33.9 and 36.8, 1000 behind 500 45.5 and 48.5; 400 behind 1100 41.4 and 39.5.
+constexpr int kKv8FewSplits = 3, kKv8Saved = 768;
 constexpr int kKv8Counters = 16384;    // split tiles of a call, at most
 
 // Splits and counters that a call can need.  A tile is split only if its
@@ -178,7 +187,8 @@ __device__ __forceinline__ bool kv8_pick(const Kv8AttnArgs& A, int entry, bool r
       tiles = mine ? (cols + TC - 1) / TC : 0;
     }
     const int p = max(per, ((len + A.max_splits - 1) / A.max_splits + 63) / 64 * 64);
-    const int splits = max(1, (len + p - 1) / p);
+    int splits = len <= kKv8Whole ? 1 : (len + p - 1) / p;
+    if (TC > 16 && splits <= kKv8FewSplits && len - p < kKv8Saved) splits = 1;
     // (row starts out of order can name rows many times over: capped, so that the
     // counts below stay in range until they are found to exceed the grid)
     const int mine = min(tiles * splits, A.entries + 1), ms = splits > 1 ? mine : 0, mu = splits > 1 ? tiles : 0;
@@ -192,7 +202,7 @@ __device__ __forceinline__ bool kv8_pick(const Kv8AttnArgs& A, int entry, bool r
       w.cols = of(cols);
       w.len = of(len);
       w.splits = of(splits);
-      const int j = entry - before - of(upto - mine), pl = of(p);
+      const int j = entry - before - of(upto - mine), pl = w.splits > 1 ? of(p) : w.len;
       // (the last tile first: of a causal sequence it sees the most)
       w.tile = of(tiles) - 1 - j / w.splits;
       w.split = j % w.splits;

@@ -38,7 +38,8 @@ inline Kv8Cut kv8_cut(const Kv8Pages& kv, int hd, int n_seqs, int n_rows, int n_
   c.pcols = c.many ? kManyCols : (int)std::min<long long>(kFewCols, std::max<long long>(1, cols));
   const long long tiles = std::min<long long>(n_seqs, n_rows) + cols / c.cols;   // at most: ceil(a) <= a + 1 where a > 0
   const long long cap = (long long)kv.mbps * kv.bs;
-  const long long most = tiles * std::min<long long>(c.max_splits, (cap + kKv8MinTokens - 1) / kKv8MinTokens);
+  const long long most =
+      tiles * (cap <= kKv8Whole ? 1 : std::min<long long>(c.max_splits, (cap + kKv8MinTokens - 1) / kKv8MinTokens));
   c.entries = std::min(most, kv8_share(c.target, H) + tiles);
   const long long slots = std::min(most, 2LL * kv8_share(c.target, H));
   c.bytes = sizeof(uint32_t) * kKv8Counters + sizeof(float) * slots * H * kv8_part_floats(c.pcols, hd);
