@@ -27,6 +27,8 @@
 // waves per SIMD); one row behind 1025 positions 10.7 us and behind 17 5.9 us, which
 // are chains: launch, lengths, block ids, codes, join.
 #pragma once
+#include <type_traits>
+
 #include "kv8_attn.h"
 
 namespace m2r2 {
@@ -371,76 +373,145 @@ __global__ __launch_bounds__(kFewThreads, 2) void k8_few(Kv8AttnArgs A, Out out)
   // ---- the waves' results, and the own key's, combined -------------------------
   float* part = A.part + ((int64_t)w.slot * A.kv.H + h) * kv8_part_floats(A.pcols, HD);
   const int64_t pstep = (int64_t)A.kv.H * kv8_part_floats(A.pcols, HD);
-  for (int e = 2 * tid; e < live * HD; e += 2 * kFewThreads) {
-    const int i = e / HD, d = e % HD;
-    const float oz = own ? oz_s[i] : -INFINITY;
-    float M = oz;
+  constexpr int kMostPairs = kFewCols * HD / 2 / kFewThreads;   // of dims, of a thread
+  auto combine = [&](auto pairs_each) {
+    constexpr int EN = decltype(pairs_each)::value;
+    float M[EN], l[EN], a[EN], b[EN];
 #pragma unroll
-    for (int x = 0; x < kFewWaves; ++x) M = fmaxf(M, m_s[x][i]);
-    float l = oz != -INFINITY ? __builtin_amdgcn_exp2f(oz - M) : 0.f;
-    float a = 0.f, b = 0.f;
-    if (l != 0.f) {
-      a = l * ov_s[i][d];
-      b = l * ov_s[i][d + 1];
-    }
+    for (int k = 0; k < EN; ++k) {
+      const int e = min(2 * (tid + k * kFewThreads), live * HD - 2), i = e / HD, d = e % HD;
+      const float oz = own ? oz_s[i] : -INFINITY;
+      M[k] = oz;
 #pragma unroll
-    for (int x = 0; x < kFewWaves; ++x) {
-      const float y = kv8_weight(m_s[x][i], l_s[x][i], M);
-      if (l_s[x][i] != 0.f) {
+      for (int x = 0; x < kFewWaves; ++x) M[k] = fmaxf(M[k], m_s[x][i]);
+      l[k] = oz != -INFINITY ? __builtin_amdgcn_exp2f(oz - M[k]) : 0.f;
+      a[k] = b[k] = 0.f;
+      if (l[k] != 0.f) {
+        a[k] = l[k] * ov_s[i][d];
+        b[k] = l[k] * ov_s[i][d + 1];
+      }
+#pragma unroll
+      for (int x = 0; x < kFewWaves; ++x) {
+        const float lx = l_s[x][i], y = kv8_weight(m_s[x][i], lx, M[k]);
         const float2 o = *(const float2*)&acc_s[x][i][d];
-        a += y * o.x;
-        b += y * o.y;
-        l += y * l_s[x][i];
+        // (a wave that has seen nothing leaves zeros)
+        a[k] += y * o.x;
+        b[k] += y * o.y;
+        l[k] += lx != 0.f ? y * lx : 0.f;
       }
     }
-    if (w.splits == 1) {
-      a = kv8_over(a, l);
-      b = kv8_over(b, l);
-      out.put(A, w.r0 + (c0 + i) / A.group, h * A.group + (c0 + i) % A.group, d, a, b);
-      if (Out::kKeep) *(float2*)&ov_s[i][d] = make_float2(a, b);   // (read above, by this thread)
-    } else {
-      float* p = part + (int64_t)w.split * pstep;
-      st_agent2(p + e, a, b);
-      if (d == 0) st_agent2(p + A.pcols * HD + 2 * i, M, l);
+#pragma unroll
+    for (int k = 0; k < EN; ++k) {
+      const int e = 2 * (tid + k * kFewThreads), i = e / HD, d = e % HD;
+      if (e >= live * HD) break;
+      if (w.splits == 1) {
+        a[k] = kv8_over(a[k], l[k]);
+        b[k] = kv8_over(b[k], l[k]);
+        out.put(A, w.r0 + (c0 + i) / A.group, h * A.group + (c0 + i) % A.group, d, a[k], b[k]);
+        if (Out::kKeep) *(float2*)&ov_s[i][d] = make_float2(a[k], b[k]);   // (read above, by this thread)
+      } else {
+        float* p = part + (int64_t)w.split * pstep;
+        st_agent2(p + e, a[k], b[k]);
+        if (d == 0) st_agent2(p + A.pcols * HD + 2 * i, M[k], l[k]);
+      }
     }
-  }
+  };
+  // (several pairs at once where a thread has them: with 16 columns one at a time takes 1 us longer)
+  if (live * HD > 2 * kFewThreads) combine(std::integral_constant<int, kMostPairs>{});
+  else combine(std::integral_constant<int, 1>{});
   if (w.splits == 1) {
     out.finish(ahead, A, w, h, live, ov_s, &mw[0][0]);
     return;
   }
   // ---- the last split to arrive joins them ---------------------------------------
   if (!arrive_last(A.cnt + w.unit * A.kv.H + h, w.splits, &last_s)) return;
-  // Pairs of dims; where a column or two leave threads over, groups of threads
-  // take every so-manieth split each.  The first loads do not wait for the weights.
-  constexpr int UN = 16;
+  // A thread takes pairs of dims: several where there are many columns, their
+  // loads together; where a column or two leave threads over, groups of threads
+  // take every so-manieth split each.  A column's weights and sum are one wave's, a
+  // lane per split.  Every load of either kind is a trip to memory, so the first
+  // ones do not wait for the weights, and those of the weights go out together:
+  // 16 columns in 8 splits 14.6 us, 16.2 with one pair and one column at a time.
   const int pairs = live * (HD / 2);
-  const int groups = pairs <= kFewThreads / 4 ? 4 : pairs <= kFewThreads / 2 ? 2 : 1;
-  const int width = kFewThreads / groups;
-  const int grp = __builtin_amdgcn_readfirstlane(tid / width), e0 = tid % width;
   auto at_split = [&](int x) { return part + (int64_t)x * pstep; };
-  float2 v[UN];
-  auto request = [&](int x, int e) {   // splits x, x + groups, ...
+  auto weights = [&]() {
+    float2 ml[kFewCols / kFewWaves];
 #pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      v[u] = make_float2(0.f, 0.f);
-      if (x + u * groups < w.splits) v[u] = ld_agent2(at_split(x + u * groups) + 2 * e);
+    for (int k = 0; k < kFewCols / kFewWaves; ++k) {
+      const int i = wv + k * kFewWaves;
+      if (i < live) ml[k] = ld_agent2(at_split(min(lane, w.splits - 1)) + A.pcols * HD + 2 * i);
     }
+#pragma unroll
+    for (int k = 0; k < kFewCols / kFewWaves; ++k) {
+      const int i = wv + k * kFewWaves;
+      if (i >= live) break;
+      const float m = lane < w.splits ? ml[k].x : -INFINITY, l = lane < w.splits ? ml[k].y : 0.f;
+      const float y = kv8_weight(m, l, wave_max(m));
+      mw[i][lane] = y;
+      const float s = wave_sum(l != 0.f ? y * l : 0.f);
+      if (lane == 0) li_s[i] = s;
+    }
+    __syncthreads();
   };
-  request(grp, min(e0, pairs - 1));
-  for (int i = wv; i < live; i += kFewWaves) {   // a wave per column, a lane per split
-    const float2 ml = ld_agent2(at_split(min(lane, w.splits - 1)) + A.pcols * HD + 2 * i);
-    const float m = lane < w.splits ? ml.x : -INFINITY, l = lane < w.splits ? ml.y : 0.f;
-    const float y = kv8_weight(m, l, wave_max(m));
-    mw[i][lane] = y;
-    const float s = wave_sum(l != 0.f ? y * l : 0.f);
-    if (lane == 0) li_s[i] = s;
-  }
-  __syncthreads();
-  for (int e = e0; e - e0 < pairs; e += width) {
-    const int ee = min(e, pairs - 1), i = 2 * ee / HD;
+  auto put = [&](int e, float a, float b) {
+    const int i = 2 * e / HD;
+    a = kv8_over(a, li_s[i]);
+    b = kv8_over(b, li_s[i]);
+    out.put(A, w.r0 + (c0 + i) / A.group, h * A.group + (c0 + i) % A.group, 2 * e - i * HD, a, b);
+    if (Out::kKeep) *(float2*)&ov_s[i][2 * e - i * HD] = make_float2(a, b);
+  };
+  auto wide = [&](auto pairs_each) {
+    constexpr int EN = decltype(pairs_each)::value, UN = EN > 2 ? 8 : 16;
+    float2 v[EN][UN], sum[EN];
+    auto request = [&](int x) {
+#pragma unroll
+      for (int u = 0; u < UN; ++u)
+#pragma unroll
+        for (int k = 0; k < EN; ++k)
+          if (x + u < w.splits) v[k][u] = ld_agent2(at_split(x + u) + 2 * min(tid + k * kFewThreads, pairs - 1));
+    };
+    request(0);
+    weights();
+#pragma unroll
+    for (int k = 0; k < EN; ++k) sum[k] = make_float2(0.f, 0.f);
+    for (int x = 0; x < w.splits; x += UN) {
+      if (x) request(x);
+#pragma unroll
+      for (int u = 0; u < UN; ++u) {
+#pragma unroll
+        for (int k = 0; k < EN; ++k) {
+          // (past the last split: weight zero)
+          const float y = mw[2 * min(tid + k * kFewThreads, pairs - 1) / HD][x + u];
+          sum[k].x += y != 0.f ? y * v[k][u].x : 0.f;
+          sum[k].y += y != 0.f ? y * v[k][u].y : 0.f;
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < EN; ++k)
+      if (tid + k * kFewThreads < pairs) put(tid + k * kFewThreads, sum[k].x, sum[k].y);
+  };
+  if (pairs > 2 * kFewThreads) {
+    wide(std::integral_constant<int, kMostPairs>{});
+  } else if (pairs > kFewThreads) {
+    wide(std::integral_constant<int, 2>{});
+  } else {
+    constexpr int UN = 16;
+    const int groups = pairs <= kFewThreads / 4 ? 4 : pairs <= kFewThreads / 2 ? 2 : 1;
+    const int width = kFewThreads / groups;
+    const int grp = __builtin_amdgcn_readfirstlane(tid / width), e = tid % width, ee = min(e, pairs - 1), i = 2 * ee / HD;
+    float2 v[UN];
+    auto request = [&](int x) {   // splits x, x + groups, ...
+#pragma unroll
+      for (int u = 0; u < UN; ++u) {
+        v[u] = make_float2(0.f, 0.f);
+        if (x + u * groups < w.splits) v[u] = ld_agent2(at_split(x + u * groups) + 2 * ee);
+      }
+    };
+    request(grp);
+    weights();
     float a = 0.f, b = 0.f;
     for (int x = grp; x < w.splits; x += UN * groups) {
-      if (x != grp || e != e0) request(x, ee);
+      if (x != grp) request(x);
 #pragma unroll
       for (int u = 0; u < UN; ++u) {
         // (past the last split: weight zero)
@@ -449,7 +520,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void k8_few(Kv8AttnArgs A, Out out)
         b += y != 0.f ? y * v[u].y : 0.f;
       }
     }
-    if (groups > 1) {   // (one turn of the loop: at most `width` pairs)
+    if (groups > 1) {
       float2* red = (float2*)&acc_s[0][0][0];
       if (e < pairs) red[grp * width + e] = make_float2(a, b);
       __syncthreads();
@@ -461,12 +532,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void k8_few(Kv8AttnArgs A, Out out)
         }
       }
     }
-    if (grp == 0 && e < pairs) {
-      a = kv8_over(a, li_s[i]);
-      b = kv8_over(b, li_s[i]);
-      out.put(A, w.r0 + (c0 + i) / A.group, h * A.group + (c0 + i) % A.group, 2 * e - i * HD, a, b);
-      if (Out::kKeep) *(float2*)&ov_s[i][2 * e - i * HD] = make_float2(a, b);
-    }
+    if (grp == 0 && e < pairs) put(e, a, b);
   }
   out.finish(ahead, A, w, h, live, ov_s, &mw[0][0]);
 }
