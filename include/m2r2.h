@@ -36,7 +36,8 @@
  *    are stored in the configured weight dtype; norm gains are always float32.
  *  - KV cache: paged, slow stream only.  K and V pages are
  *    [n_layers][num_blocks][n_heads][block_size][head_dim] in the configured
- *    KV dtype (M2R2_FP8: bytes, with scales [n_layers][num_blocks][n_heads]); block_table is [batch][max_blocks_per_seq] int32 (physical
+ *    KV dtype (M2R2_FP8: bytes, with scales [n_layers][num_blocks][n_heads]);
+ *    block_table is [batch][max_blocks_per_seq] int32 (physical
  *    block of each logical block, shared by all layers).  Positions outside a
  *    sequence's block table are not read or written (a sticky device error
  *    bit is set instead).
@@ -176,7 +177,8 @@ typedef struct {
   const int32_t* block_table_d;  /* [batch][max_blocks_per_seq] */
   int32_t* seq_lens_d;           /* [batch]: written with the number of valid cache positions */
   int32_t num_blocks, block_size, max_blocks_per_seq;
-  /* M2R2_FP8 only (not read otherwise): [n_layers][num_blocks][n_heads]; block_size is then a multiple of 16, at most 256 */
+  /* M2R2_FP8 only (not read otherwise): [n_layers][num_blocks][n_heads];
+   * block_size is then a multiple of 16, at most 256 */
   float* k_scales;
   float* v_scales;
 } m2r2_kv;

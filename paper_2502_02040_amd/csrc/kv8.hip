@@ -160,9 +160,11 @@ M2R2_API m2r2_status m2r2_kv8_append(const m2r2_kv8* kv, const m2r2_kv8_rows* r,
   if (r->n_heads) {
     if (m2r2_status s = check_heads(kv, r->n_heads)) return s;
     if (m2r2_status s = check_array("q", r->q, r->n_rows, r->n_heads, r->q_row, r->q_head, r->dtype)) return s;
-    if (m2r2_status s = check_written("q_out", r->q_out, r->n_rows, r->n_heads, r->qo_row, r->qo_head, kv->head_dim, r->dtype))
+    if (m2r2_status s = check_written("q_out", r->q_out, r->n_rows, r->n_heads, r->qo_row, r->qo_head, kv->head_dim,
+                                      r->dtype))
       return s;
-    if (r->q == r->q_out && ((r->n_rows > 1 && r->q_row != r->qo_row) || (r->n_heads > 1 && r->q_head != r->qo_head)))
+    if (r->q == r->q_out &&
+        ((r->n_rows > 1 && r->q_row != r->qo_row) || (r->n_heads > 1 && r->q_head != r->qo_head)))
       return set_error(M2R2_E_INVALID, "q_out is q with other strides");
   } else if (r->q || r->q_out) {
     return set_error(M2R2_E_INVALID, "q or q_out given with n_heads 0");
@@ -211,12 +213,14 @@ M2R2_API m2r2_status m2r2_kv8_attention(const m2r2_kv8* kv, const m2r2_kv8_query
   size_t need = 0;
   if (m2r2_status s = m2r2_kv8_workspace_size(kv, a->n_seqs, a->n_rows, a->n_heads, &need)) return s;
   if (m2r2_status s = check_array("q", a->q, a->n_rows, a->n_heads, a->q_row, a->q_head, a->dtype)) return s;
-  if (m2r2_status s = check_written("out", a->out, a->n_rows, a->n_heads, a->out_row, a->out_head, kv->head_dim, a->dtype))
+  if (m2r2_status s = check_written("out", a->out, a->n_rows, a->n_heads, a->out_row, a->out_head, kv->head_dim,
+                                    a->dtype))
     return s;
   if (a->own_d) {
     if (a->n_own < 1) return set_error(M2R2_E_SHAPE, "n_own %d", a->n_own);
-    if (m2r2_status s = check_array("own_k", a->own_k, a->n_own, kv->n_kv_heads, a->ok_row, a->ok_head, a->dtype)) return s;
-    if (m2r2_status s = check_array("own_v", a->own_v, a->n_own, kv->n_kv_heads, a->ov_row, a->ov_head, a->dtype)) return s;
+    const int H = kv->n_kv_heads;
+    if (m2r2_status s = check_array("own_k", a->own_k, a->n_own, H, a->ok_row, a->ok_head, a->dtype)) return s;
+    if (m2r2_status s = check_array("own_v", a->own_v, a->n_own, H, a->ov_row, a->ov_head, a->dtype)) return s;
   }
   if (!(a->scale >= 0.f) || a->scale > 3e38f) return set_error(M2R2_E_INVALID, "scale");
   if (!workspace || !aligned(workspace, 256)) return set_error(M2R2_E_INVALID, "workspace NULL or not 256-byte aligned");

@@ -163,19 +163,19 @@ __global__ __launch_bounds__(kKv8AppThreads) void k8_append(Kv8AppArgs A) {
         // (two heads' loads ahead of their arithmetic: 82 us for the prompt above, 86 for one head's, 84 for four)
         for (int ha = h0; ha < h1; ha += 2) {
           Kv8Raw<BF> lo[2], hi[2];
-  #pragma unroll
+#pragma unroll
           for (int g = 0; g < 2; ++g) {
             if (ha + g >= h1) break;
             const int64_t at = (row_b + slot) * A.q_row + (int64_t)(ha + g) * A.q_head + d;
             lo[g].load(A.q, at);
             hi[g].load(A.q, at + HALF);
           }
-  #pragma unroll
+#pragma unroll
           for (int g = 0; g < 2; ++g) {
             const int h = ha + g;
             if (h >= h1) break;
             float y0[8], y1[8];
-  #pragma unroll
+#pragma unroll
             for (int x = 0; x < 8; ++x) {
               y0[x] = lo[g].at(x);
               y1[x] = hi[g].at(x);
@@ -185,12 +185,12 @@ __global__ __launch_bounds__(kKv8AppThreads) void k8_append(Kv8AppArgs A) {
               }
             }
             const int64_t to = (row_b + slot) * A.qo_row + (int64_t)h * A.qo_head + d;
-  #pragma unroll
+#pragma unroll
             for (int z = 0; z < 2; ++z) {
               const float(&y)[8] = z ? y1 : y0;
               if constexpr (BF) {
                 bf16x8_t o;
-  #pragma unroll
+#pragma unroll
                 for (int x = 0; x < 8; ++x) o[x] = (__bf16)y[x];
                 *(bf16x8_t*)((uint16_t*)A.qo + to + z * HALF) = o;
               } else {

@@ -12,11 +12,13 @@
 //     operand of O^T = V^T P^T as it stands.
 //   * Two workgroups per compute unit, so that one's softmax runs beside the
 //     other's products.
-// Measured (bfloat16, 32 heads of 128 for 8): two prompts of 4001 rows 171 us, 0.78
-// PFLOP/s of the 1.31 that a large library product reaches here; 500 rows behind
-// 8500 positions 101 us, 0.71 PFLOP/s, the join's launch included (5 us, also where
-// nothing is split; a join inside this kernel took 106 and 162 us, but 69 instead
-// of 20 for 8 rows behind 8000 positions).
+// Measured (bfloat16, 32 heads of 128 for 8): prompts of 4001 and of 500 rows 167 us,
+// 0.80 PFLOP/s of the 1.31 that a large library product reaches here; 500 rows behind
+// 8500 positions 98 us, 0.73 PFLOP/s, the join's launch included (11 us there, 4.5
+// where nothing is split; a join inside this kernel took 106 and 162 us, but 69
+// instead of 20 for 8 rows behind 8000 positions).  Counters of the prompts: the matrix
+// unit busy 34 % of the time, the vector unit 45 %, the LDS 37 %; what one of two
+// waves on a SIMD issues seldom overlaps the other's products.
 // Probabilities of bfloat16 rows are rounded to bfloat16 (half a step of 2^-8, of
 // the same size as the result's own rounding, and averaged over the positions):
 // a second part would cost half of all products again.  Those of float32 rows

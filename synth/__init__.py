@@ -37,7 +37,7 @@ class ModelConfig:
     """Shape and storage precision of a decoder-only transformer with an
     accelerated residual stream.
 
-    ``wdtype``/``kvdtype`` are ``"f32"`` or ``"bf16"``.  ``n_experts == 0``
+    ``wdtype``/``kvdtype`` are ``"f32"`` or ``"bf16"``, ``kvdtype`` also ``"fp8"``.  ``n_experts == 0``
     means a dense SwiGLU MLP of width ``ffn``; otherwise each layer holds
     ``n_experts`` SwiGLU experts of width ``expert_ffn`` with top-``top_k``
     routing, and the accelerated stream uses a rank-``rank`` adapter in place
