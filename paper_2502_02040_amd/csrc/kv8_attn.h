@@ -160,14 +160,24 @@ __device__ __forceinline__ void kv8_seq(const Kv8AttnArgs& A, int s, bool report
 // positions 17.1 us in splits of 512, 20.9 in splits of 256; four of 8192 15.9 and
 // 18.7; where the share is longer than that, a share of 768 workgroups against
 // one of 256: eight sequences of 4096 (32 heads of 96) 27.8 and 32.5.
-__device__ __forceinline__ int kv8_split_len(const Kv8AttnArgs& A, float sum) {
+//
+// k8_many's workgroups hold a compute unit to themselves or in pairs, and a few
+// more than fit double the time: there a tile is cut into as many splits as
+// leave the total within the target (FEWER), not one more.
+struct Kv8Split {
+  int per;       // positions of a split
+  float share;   // of all positions, of a workgroup
+};
+__device__ __forceinline__ Kv8Split kv8_split(const Kv8AttnArgs& A, float sum) {
   // (a little more than the share: the float sum may be that much too small)
   const float all = min(sum * (float)A.kv.H * 1.002f, 1e18f);
-  const float share = max(all / (float)A.target, min(all / (float)kKv8Units, (float)kKv8FullTokens));
-  return max(kKv8MinTokens, ((int)min(share, 1e9f) + 63) / 64 * 64);
+  const float least = max((float)kKv8MinTokens, min(all / (float)kKv8Units, (float)kKv8FullTokens));
+  const float share = all / (float)A.target;
+  return {((int)min(max(share, least), 1e9f) + 63) / 64 * 64, share >= least ? share : 0.f};
 }
 template <int TC>
 __device__ __forceinline__ bool kv8_pick(const Kv8AttnArgs& A, int entry, bool report, Kv8Work& w) {
+  constexpr bool FEWER = TC > 16;   // k8_many
   const int lane = threadIdx.x & 63;
   float sum = 0.f;
   int r0 = 0, cols = 0, len = 0, tiles = 0;
@@ -177,7 +187,7 @@ __device__ __forceinline__ bool kv8_pick(const Kv8AttnArgs& A, int entry, bool r
     tiles = mine ? (cols + TC - 1) / TC : 0;
     sum += (float)tiles * (float)len;
   }
-  const int per = kv8_split_len(A, wave_sum(sum));
+  const Kv8Split cut = kv8_split(A, wave_sum(sum));
   int before = 0, slots = 0, units = 0;
   w.s = -1;
   for (int c = 0; c < A.n_seqs; c += 64) {
@@ -186,9 +196,13 @@ __device__ __forceinline__ bool kv8_pick(const Kv8AttnArgs& A, int entry, bool r
       kv8_seq<TC>(A, mine ? c + lane : A.n_seqs - 1, false, r0, cols, len);
       tiles = mine ? (cols + TC - 1) / TC : 0;
     }
-    const int p = max(per, ((len + A.max_splits - 1) / A.max_splits + 63) / 64 * 64);
+    int p = max(cut.per, ((len + A.max_splits - 1) / A.max_splits + 63) / 64 * 64);
+    if (FEWER && cut.share > 0.f) {
+      const int n = max(1, min(A.max_splits, (int)((float)len * 1.004f / cut.share)));
+      p = ((len + n - 1) / n + 63) / 64 * 64;
+    }
     int splits = len <= kKv8Whole ? 1 : (len + p - 1) / p;
-    if (TC > 16 && splits <= kKv8FewSplits && len - p < kKv8Saved) splits = 1;
+    if (FEWER && splits <= kKv8FewSplits && len - p < kKv8Saved) splits = 1;
     // (row starts out of order can name rows many times over: capped, so that the
     // counts below stay in range until they are found to exceed the grid)
     const int mine = min(tiles * splits, A.entries + 1), ms = splits > 1 ? mine : 0, mu = splits > 1 ? tiles : 0;

@@ -18,21 +18,22 @@ struct Kv8Cut {
 };
 
 // Up to this many columns a sequence on average, k8_few, which reads the cache
-// once for every sixteen; above, k8_many with its second launch.  Measured at 8
-// heads of 128 for 4 (us, k8_few and k8_many): one sequence of 1500 positions, 32
-// columns 18.2 and 15.4, 64 17.8 and 16.7; four of 8000, 32 columns 28.8 and 29.2, 64
-// 40.7 and 35.7; in float32, whose products are threefold, four of 8000 with 64
-// columns 34.7 and 63.9, 128 71.2 and 71.9, 256 95.5 and 80.4.
-constexpr int kv8_few_most(bool bf16) { return bf16 ? 32 : 96; }
+// once for every sixteen; above, k8_many, whose tiles would not be filled below, with
+// its second launch.  Measured at 8 heads of 128 for 4 with 64, 128 and 256 columns (us,
+// k8_few / k8_many): one sequence of 400 positions 10.2/17.3, 10.2/19.4, 10.3/19.4; of
+// 1500 14.5/16.0, 15.4/20.4, 19.6/22.9; four of 1000 14.9/24.2, 16.9/30.4, 24.5/31.5; four
+// of 8000 36.1/45.3, 53.0/51.8, 81.2/54.1, in float32 31.8/54.1, 65.3/61.2, 91.7/83.7.  One
+// sequence of 8000 would gain from fewer: 24.7/21.2, 37.0/24.8, 48.8/28.7.
+constexpr int kFewMost = 128;
 
 inline Kv8Cut kv8_cut(const Kv8Pages& kv, int hd, int n_seqs, int n_rows, int n_heads, bool bf16) {
   Kv8Cut c;
   const int H = kv.H, group = n_heads / H;
   const long long cols = (long long)n_rows * group;
-  c.many = cols > (long long)kv8_few_most(bf16) * std::max(1, n_seqs);
+  c.many = cols > (long long)kFewMost * std::max(1, n_seqs);
   c.cols = c.many ? kManyCols : kFewCols;
-  // what a compute unit holds: two workgroups, three of k8_few's bfloat16 form
-  c.target = (c.many || !bf16 ? 2 : 3) * kKv8Units;
+  // what a compute unit holds: two workgroups, three of k8_few's bfloat16 form, one of k8_many's float32 form
+  c.target = (c.many == bf16 ? 2 : bf16 ? 3 : c.many ? 1 : 2) * kKv8Units;
   // joins cost a little per split: 32, or what gives every compute unit one
   c.max_splits = (int)std::max(32LL, std::min<long long>(kKv8MaxSplits, kKv8Units / std::max(1LL, (long long)n_seqs * H)));
   c.pcols = c.many ? kManyCols : (int)std::min<long long>(kFewCols, std::max<long long>(1, cols));
