@@ -7,7 +7,8 @@ given, whichever device is current.
 from __future__ import annotations
 
 import ctypes
-from ctypes import POINTER, c_float, c_int32, c_int64, c_size_t, c_void_p
+import struct
+from ctypes import POINTER, c_char_p, c_float, c_int32, c_int64, c_size_t, c_void_p
 from typing import Optional
 
 from .binding import BF16, F32, _check, lib
@@ -40,7 +41,26 @@ class _Query(ctypes.Structure):
                 ("out_head", c_int64), ("err_d", c_void_p)]
 
 
+# The last two as struct formats (native alignment): filling one takes a quarter of
+# the time of building the ctypes structure.
+_ROWS = struct.Struct("@iiPPiPPqqqqPiiPPqqqqP")
+_QUERY = struct.Struct("@iiPPPiiPqqPPPiqqqqfPqqP")
+
 _fns = None
+_packed_fns = None
+
+
+def _packed():
+    """(append, attention) that take descriptions as bytes."""
+    global _packed_fns
+    if _packed_fns is None:
+        L = lib()
+        append, attention = L["m2r2_kv8_append"], L["m2r2_kv8_attention"]   # (function objects of their own)
+        append.argtypes = [c_char_p, c_char_p, c_void_p]
+        attention.argtypes = [c_char_p, c_char_p, c_void_p, c_size_t, c_void_p]
+        append.restype = attention.restype = c_int32
+        _packed_fns = (append, attention)
+    return _packed_fns
 
 
 def _lib():
@@ -85,6 +105,7 @@ class KV8Pages:
         self.n_seqs, self.n_kv_heads, self.head_dim = block_table.shape[0], H, hd
         self._desc = _Pages(k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
                             block_table.data_ptr(), nb, bs, block_table.shape[1], H, hd)
+        self._bytes = bytes(self._desc)
 
 
 _torch = None
@@ -102,24 +123,24 @@ def _t():
 # A decoding step makes these calls for every layer, and its kernels take a few
 # microseconds each: the checks below look at every tensor once.
 
-def _int32s(t, n: int, name: str, gpu: int) -> Optional[int]:
-    """Pointer to a vector of at least n int32 on the GPU (None: NULL)."""
+def _int32s(t, n: int, name: str, gpu: int) -> int:
+    """Pointer to a vector of at least n int32 on the GPU (None: 0)."""
     if t is None:
-        return None
-    sh = t.shape
-    if len(sh) != 1 or sh[0] < n or t.dtype is not _t().int32 or t.stride()[0] != 1 or t.get_device() != gpu:
+        return 0
+    if t.dim() != 1 or t.numel() < n or t.dtype is not _t().int32 or not t.is_contiguous() or t.get_device() != gpu:
         raise ValueError(f"{name}: a contiguous int32 vector of at least {n} entries on GPU {gpu}, "
-                         f"not {t.dtype} {tuple(sh)} on {t.device}")
+                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _rows(t, name: str, n: int, heads: int, hd: int, dtype, gpu: int):
+def _rows(t, name: str, shape: tuple, dtype, gpu: int):
     """(pointer, row stride, head stride) of a [n][heads][hd] tensor."""
-    row, head, dim = t.stride() if t.dim() == 3 else (0, 0, 0)
-    if t.shape != (n, heads, hd) or dim != 1 or t.dtype is not dtype or t.get_device() != gpu:
-        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, strides {tuple(t.stride())} on {t.device}; "
-                         f"expected {dtype} ({n}, {heads}, {hd}) with adjacent dims on GPU {gpu}")
-    return t.data_ptr(), row, head
+    if t.shape == shape and t.dtype is dtype and t.get_device() == gpu:
+        row, head, dim = t.stride()
+        if dim == 1:
+            return t.data_ptr(), row, head
+    raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, strides {tuple(t.stride())} on {t.device}; "
+                     f"expected {dtype} {shape} with adjacent dims on GPU {gpu}")
 
 
 def _dtype(t, name: str):
@@ -134,17 +155,17 @@ def _dtype(t, name: str):
 
 def _call(fn, where: str, kv, stream, *args) -> None:
     """fn(*args, stream) with the cache's GPU current."""
-    gpu, cuda = kv.gpu, _t().cuda
+    gpu, torch = kv.gpu, _t()
     if gpu < 0:
         raise ValueError(f"{where}: tensors on {kv.device}")
     if stream is not None:
         s = stream.cuda_stream
     else:   # (the handle without a Stream object around it, which takes a microsecond)
-        s = _t()._C._cuda_getCurrentRawStream(gpu)
-    if cuda.current_device() == gpu:
+        s = torch._C._cuda_getCurrentRawStream(gpu)
+    if torch._C._cuda_getDevice() == gpu:
         st = fn(*args, s)
     else:
-        with cuda.device(gpu):
+        with torch.cuda.device(gpu):
             st = fn(*args, s)
     if st:
         _check(st, where)
@@ -159,26 +180,28 @@ def kv8_append(kv: KV8Pages, k, v, row_start, positions, *, rope=None, q=None, q
     ``errors``: an int32 tensor into which the kernels or error bits."""
     n, H, hd, ns, gpu = len(k), kv.n_kv_heads, kv.head_dim, kv.n_seqs, kv.gpu
     code, dt = _dtype(k, "k")
-    kp, k_row, k_head = _rows(k, "k", n, H, hd, dt, gpu)
-    vp, v_row, v_head = _rows(v, "v", n, H, hd, dt, gpu)
-    heads, qp, q_row, q_head, op, o_row, o_head = 0, None, 0, 0, None, 0, 0
+    shape = (n, H, hd)
+    kp, k_row, k_head = _rows(k, "k", shape, dt, gpu)
+    vp, v_row, v_head = _rows(v, "v", shape, dt, gpu)
+    heads, qp, q_row, q_head, op, o_row, o_head = 0, 0, 0, 0, 0, 0, 0
     if q is not None and q_out is not None:
         heads = q.shape[1] if q.dim() == 3 else 0
-        qp, q_row, q_head = _rows(q, "q", n, heads, hd, dt, gpu)
-        op, o_row, o_head = _rows(q_out, "q_out", n, heads, hd, dt, gpu)
+        shape = (n, heads, hd)
+        qp, q_row, q_head = _rows(q, "q", shape, dt, gpu)
+        op, o_row, o_head = (qp, q_row, q_head) if q_out is q else _rows(q_out, "q_out", shape, dt, gpu)
     elif q is not None or q_out is not None:
         raise ValueError("q and q_out come together")
-    rp, rlen = None, 0
+    rp, rlen = 0, 0
     if rope is not None:
-        rlen = rope.shape[0]
+        rlen = len(rope)
         if (rope.shape != (rlen, hd // 2, 2) or rope.dtype is not _t().float32 or not rope.is_contiguous()
                 or rope.get_device() != gpu):
             raise ValueError("rope: a contiguous float32 tensor [length][head_dim/2][2] on the cache's GPU")
         rp = rope.data_ptr()
-    r = _Rows(ns, n, _int32s(row_start, ns + 1, "row_start", gpu), _int32s(positions, ns, "positions", gpu), code, kp, vp,
-              k_row, k_head, v_row, v_head, rp, rlen, heads, qp, op, q_row, q_head, o_row, o_head,
-              _int32s(errors, 1, "errors", gpu))
-    _call(_lib()[0], "m2r2_kv8_append", kv, stream, kv._desc, r)
+    r = _ROWS.pack(ns, n, _int32s(row_start, ns + 1, "row_start", gpu), _int32s(positions, ns, "positions", gpu), code,
+                   kp, vp, k_row, k_head, v_row, v_head, rp, rlen, heads, qp, op, q_row, q_head, o_row, o_head,
+                   _int32s(errors, 1, "errors", gpu))
+    _call(_packed()[0], "m2r2_kv8_append", kv, stream, kv._bytes, r)
 
 
 def kv8_workspace(kv: KV8Pages, q):
@@ -203,20 +226,21 @@ def kv8_attention(kv: KV8Pages, q, row_start, lens, out, workspace, *, visible=N
     if scale is not None and not scale > 0:
         raise ValueError(f"scale {scale}")
     code, dt = _dtype(q, "q")
-    qp, q_row, q_head = _rows(q, "q", n, heads, hd, dt, gpu)
-    op, o_row, o_head = _rows(out, "out", n, heads, hd, dt, gpu)
-    n_own, kp, k_row, k_head, vp, v_row, v_head = 0, None, 0, 0, None, 0, 0
+    shape = (n, heads, hd)
+    qp, q_row, q_head = _rows(q, "q", shape, dt, gpu)
+    op, o_row, o_head = _rows(out, "out", shape, dt, gpu)
+    n_own, wp, kp, k_row, k_head, vp, v_row, v_head = 0, 0, 0, 0, 0, 0, 0, 0
     if own is not None and own_k is not None and own_v is not None:
-        n_own = own_k.shape[0]
-        kp, k_row, k_head = _rows(own_k, "own_k", n_own, H, hd, dt, gpu)
-        vp, v_row, v_head = _rows(own_v, "own_v", n_own, H, hd, dt, gpu)
-        own = own if n_own else None
+        n_own = len(own_k)
+        shape = (n_own, H, hd)
+        kp, k_row, k_head = _rows(own_k, "own_k", shape, dt, gpu)
+        vp, v_row, v_head = _rows(own_v, "own_v", shape, dt, gpu)
+        wp = _int32s(own, n, "own", gpu) if n_own else 0
     elif own is not None or own_k is not None or own_v is not None:
         raise ValueError("own, own_k and own_v come together")
     if workspace.get_device() != gpu or not workspace.is_contiguous():
         raise ValueError(f"workspace: a contiguous tensor on GPU {gpu}")
-    a = _Query(ns, n, _int32s(row_start, ns + 1, "row_start", gpu), _int32s(lens, ns, "lens", gpu),
-               _int32s(visible, n, "visible", gpu), code, heads, qp, q_row, q_head, _int32s(own, n, "own", gpu), kp, vp,
-               n_own, k_row, k_head, v_row, v_head, 0.0 if scale is None else scale, op, o_row, o_head,
-               _int32s(errors, 1, "errors", gpu))
-    _call(_lib()[2], "m2r2_kv8_attention", kv, stream, kv._desc, a, workspace.data_ptr(), workspace.nbytes)
+    a = _QUERY.pack(ns, n, _int32s(row_start, ns + 1, "row_start", gpu), _int32s(lens, ns, "lens", gpu),
+                    _int32s(visible, n, "visible", gpu), code, heads, qp, q_row, q_head, wp, kp, vp, n_own, k_row, k_head,
+                    v_row, v_head, 0.0 if scale is None else scale, op, o_row, o_head, _int32s(errors, 1, "errors", gpu))
+    _call(_packed()[1], "m2r2_kv8_attention", kv, stream, kv._bytes, a, workspace.data_ptr(), workspace.nbytes)

@@ -87,6 +87,15 @@ def test_nothing_to_do_is_no_error():
     assert attention(_pages(), _query(n_seqs=0), P, 1 << 40, None) == 0
 
 
+def test_packed_descriptions_are_the_structures():
+    """The binding's struct formats lay out what the ctypes structures do."""
+    for fmt, kind in ((kv8._ROWS, kv8._Rows), (kv8._QUERY, kv8._Query)):
+        values = [0.5 if t is ctypes.c_float else i + 1 for i, (_, t) in enumerate(kind._fields_)]
+        got = kind.from_buffer_copy(fmt.pack(*values))
+        assert ctypes.sizeof(kind) == fmt.size and [getattr(got, n) for n, _ in kind._fields_] == values
+    assert bytes(_pages()) == bytes(kv8._Pages.from_buffer_copy(bytes(_pages())))
+
+
 def test_empty_calls_need_no_arrays():
     """A step without rows or without sequences: torch's empty tensors have no address."""
     append, size, attention = kv8._lib()
