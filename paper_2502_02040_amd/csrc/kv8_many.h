@@ -12,10 +12,10 @@
 //     operand of O^T = V^T P^T as it stands.
 //   * Two workgroups per compute unit, so that one's softmax runs beside the
 //     other's products.
-// Measured (bfloat16, 32 heads of 128 for 8): prompts of 4001 and of 500 rows 167 us,
-// 0.80 PFLOP/s of the 1.31 that a large library product reaches here; 500 rows behind
-// 8500 positions 98 us, 0.73 PFLOP/s, the join's launch included (11 us there, 4.5
-// where nothing is split; a join inside this kernel took 106 and 162 us, but 69
+// Measured (bfloat16, 32 heads of 128 for 8): prompts of 4001 and of 500 rows 165 us,
+// 0.81 PFLOP/s of the 1.31 that a large library product reaches here; 500 rows behind
+// 8500 positions 95 us, 0.76 PFLOP/s, the join's launch included (4.5 us where
+// nothing is split; a join inside this kernel took 106 and 162 us, but 69
 // instead of 20 for 8 rows behind 8000 positions).  Counters of the prompts: the matrix
 // unit busy 34 % of the time, the vector unit 45 %, the LDS 37 %; what one of two
 // waves on a SIMD issues seldom overlaps the other's products.
@@ -482,39 +482,69 @@ __global__ __launch_bounds__(kManyThreads) void k8_join(Kv8AttnArgs A) {
   const int groups = (live + 31) / 32;   // of 32 columns
   if (tid < 32 * groups) {
     float M = -INFINITY, l = 0.f;
+    constexpr int KEEP = 8;   // splits whose maxima and sums are read once
+    float2 keep[KEEP];
+    auto at = [&](int x) { return *(const float2*)(part + x * pstep + kManyCols * HD + 2 * tid); };
+#pragma unroll
+    for (int x = 0; x < KEEP; ++x) keep[x] = at(min(x, w.splits - 1));
+#pragma unroll
+    for (int x = 0; x < KEEP; ++x) M = fmaxf(M, keep[x].x);
 #pragma unroll 8
-    for (int x = 0; x < w.splits; ++x) M = fmaxf(M, part[x * pstep + kManyCols * HD + 2 * tid]);
-#pragma unroll 4
-    for (int x = 0; x < w.splits; ++x) {
-      const float2 t = *(const float2*)(part + x * pstep + kManyCols * HD + 2 * tid);
+    for (int x = KEEP; x < w.splits; ++x) M = fmaxf(M, at(x).x);
+    auto weigh = [&](int x, float2 t) {
       const float y = kv8_weight(t.x, t.y, M);
       y_s[x][tid] = y;
       if (t.y != 0.f) l += y * t.y;
-    }
+    };
+#pragma unroll
+    for (int x = 0; x < KEEP; ++x)
+      if (x < w.splits) weigh(x, keep[x]);
+#pragma unroll 4
+    for (int x = KEEP; x < w.splits; ++x) weigh(x, at(x));
     l_s[tid] = l;
   }
   __syncthreads();
   const int all = groups * NCH, from = all * w.split / w.splits, to = all * (w.split + 1) / w.splits;
-  for (int ch = from + wv; ch < to; ch += 4) {
-    const int g = ch / NCH, d = ch % NCH / 4, r4 = ch % 4, c = 32 * g + n;
-    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-    for (int x = 0; x < w.splits; ++x) {
-      const float4 v = *(const float4*)(part + x * pstep + ch * 256 + 4 * lane);
-      const float y = y_s[x][c];   // (zero, times zeros, for a split that the column saw nothing of)
-      a.x += y * v.x;
-      a.y += y * v.y;
-      a.z += y * v.z;
-      a.w += y * v.w;
+  // Four pieces of a wave at a time, so that a few splits keep enough loads in
+  // flight (130 rows behind 870 positions 26.1 -> 22.4 us); one where there is no more.
+  auto join = [&](auto pieces) KV8_INLINE {
+    constexpr int NP = decltype(pieces)::value, UN = NP > 1 ? 4 : 8;
+    for (int first = from + wv; first < to; first += 4 * NP) {
+      float4 a[NP];
+      int ch[NP], col[NP];
+#pragma unroll
+      for (int k = 0; k < NP; ++k) {
+        a[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        ch[k] = min(first + 4 * k, to - 1);
+        col[k] = 32 * (ch[k] / NCH) + n;
+      }
+#pragma unroll UN
+      for (int x = 0; x < w.splits; ++x) {
+#pragma unroll
+        for (int k = 0; k < NP; ++k) {
+          const float4 v = *(const float4*)(part + x * pstep + ch[k] * 256 + 4 * lane);
+          const float y = y_s[x][col[k]];   // (zero, times zeros, for a split that the column saw nothing of)
+          a[k].x += y * v.x;
+          a[k].y += y * v.y;
+          a[k].z += y * v.z;
+          a[k].w += y * v.w;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < NP; ++k) {
+        if (first + 4 * k >= to || col[k] >= live) continue;
+        const int c = col[k], d = ch[k] % NCH / 4, r4 = ch[k] % 4;
+        const float l = l_s[c];
+        const int row = w.r0 + (c0 + c) / A.group, head = h * A.group + (c0 + c) % A.group;
+        const int64_t o = (int64_t)row * A.out_row + (int64_t)head * A.out_head + 32 * d + 8 * r4 + 4 * hi;
+        const float4 z = make_float4(kv8_over(a[k].x, l), kv8_over(a[k].y, l), kv8_over(a[k].z, l), kv8_over(a[k].w, l));
+        if constexpr (BF) *(u32x2_t*)((uint16_t*)A.out + o) = u32x2_t{kv8_pk(z.x, z.y), kv8_pk(z.z, z.w)};
+        else *(float4*)((float*)A.out + o) = z;
+      }
     }
-    if (c >= live) continue;
-    const float l = l_s[c];
-    const int row = w.r0 + (c0 + c) / A.group, head = h * A.group + (c0 + c) % A.group;
-    const int64_t o = (int64_t)row * A.out_row + (int64_t)head * A.out_head + 32 * d + 8 * r4 + 4 * hi;
-    a = make_float4(kv8_over(a.x, l), kv8_over(a.y, l), kv8_over(a.z, l), kv8_over(a.w, l));
-    if constexpr (BF) *(u32x2_t*)((uint16_t*)A.out + o) = u32x2_t{kv8_pk(a.x, a.y), kv8_pk(a.z, a.w)};
-    else *(float4*)((float*)A.out + o) = a;
-  }
+  };
+  if (to - from > 4) join(std::integral_constant<int, 4>{});
+  else join(std::integral_constant<int, 1>{});
 }
 
 #undef KV8_INLINE
